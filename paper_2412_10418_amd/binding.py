@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(HERE, "_lib", "libcdsl.so")
 CDSL_OK, CDSL_EINVAL, CDSL_ERANGE, CDSL_ENOMEM, CDSL_EDEVICE, CDSL_ESTATE = 0, -1, -2, -3, -4, -5
 CDSL_F32, CDSL_BF16 = 0, 1
 CDSL_EPI_STORE, CDSL_EPI_RESIDUAL = 0, 1
+CDSL_KVQ_INT8, CDSL_KVQ_E4M3 = 0, 1
+CDSL_KVQ_PAGE, CDSL_TREE_MAX, CDSL_ACCEPT_MAX_VOCAB = 32, 512, 1 << 20
 ERR_NAMES = {0: "OK", -1: "EINVAL", -2: "ERANGE", -3: "ENOMEM", -4: "EDEVICE", -5: "ESTATE"}
 
 EXPORTS = [
@@ -32,6 +34,8 @@ EXPORTS = [
     "cdsl_prefix_lengths",
     "cdsl_free_prefix", "cdsl_destroy", "cdsl_last_error", "cdsl_profile_enable", "cdsl_profile_read",
     "cdsl_op_gemm_workspace", "cdsl_op_gemm", "cdsl_op_gemm_static", "cdsl_op_logit_rows",
+    "cdsl_op_kvq_pool_bytes", "cdsl_op_kvq_write", "cdsl_op_kvq_read", "cdsl_op_kvq_keep",
+    "cdsl_op_tree_attention_workspace", "cdsl_op_tree_attention", "cdsl_op_tree_accept",
 ]
 
 
@@ -66,6 +70,12 @@ class Limits(C.Structure):
                 ("max_d", C.c_int32), ("max_prompt", C.c_int32), ("max_prefixes", C.c_int32)]
 
 
+class KVQ(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("table", C.c_void_p), ("n_layers", C.c_int32), ("pages", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("batch", C.c_int32), ("table_stride", C.c_int32),
+                ("format", C.c_int32)]
+
+
 _lib = None
 
 
@@ -78,7 +88,7 @@ def lib():
         raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                            "`python -m paper_2412_10418_amd.build` (no CPU fallback exists)")
     L = C.CDLL(LIB_PATH)
-    vp, i32, f32 = C.c_void_p, C.c_int32, C.c_float
+    vp, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
     sig = {
         "cdsl_init": ([C.POINTER(Model), C.POINTER(Model), C.POINTER(Limits), vp, C.POINTER(vp)], i32),
         "cdsl_prefill": ([vp, vp, i32, i32, i32, C.POINTER(vp), vp, vp], i32),
@@ -118,6 +128,14 @@ def lib():
         "cdsl_op_gemm": ([vp, vp, vp, i32, i32, i32, i32, i32, vp, C.c_size_t, vp], i32),
         "cdsl_op_gemm_static": ([vp, vp, vp, i32, i32, i32, i32, i32, vp], i32),
         "cdsl_op_logit_rows": ([vp, i32, i32, vp, i32, vp, vp, vp, vp, vp], i32),
+        "cdsl_op_kvq_pool_bytes": ([i32, i32, i32, i32], C.c_size_t),
+        "cdsl_op_kvq_write": ([vp, i32, vp, vp, i32, i32, i64, i64, i64, i64, vp, vp, vp], i32),
+        "cdsl_op_kvq_read": ([vp, i32, vp, vp, i32, i32, vp, vp, vp], i32),
+        "cdsl_op_kvq_keep": ([vp, vp, vp, vp, i32, vp, vp], i32),
+        "cdsl_op_tree_attention_workspace": ([i32, i32, i32, i32, i32, i32], C.c_size_t),
+        "cdsl_op_tree_attention": ([vp, i32, vp, i32, i32, i32, i64, i64, vp, vp, vp, f32, i32, vp, vp, C.c_size_t,
+                                    vp], i32),
+        "cdsl_op_tree_accept": ([vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -250,6 +268,173 @@ def cdsl_op_soft_rows(target_logits: torch.Tensor, draft_logits: torch.Tensor, d
                                  dlp.data_ptr(), rid.data_ptr(), rlp.data_ptr(), _stream())
     _check(rc)
     return dlp, rid, rlp
+
+
+# ---------------------------------------------------------------------------
+# a drafted tree served from an 8-bit paged cache
+# ---------------------------------------------------------------------------
+_KVQ_FORMATS = {"int8": CDSL_KVQ_INT8, "e4m3": CDSL_KVQ_E4M3}
+_ROW_TYPES = {torch.float32: CDSL_F32, torch.bfloat16: CDSL_BF16}
+
+
+def _ints(t: Optional[torch.Tensor], shape, dev, name):
+    """Pointer of an int32 tensor of this shape on this device (None: null)."""
+    return _of(t, shape, torch.int32, dev, name) if t is not None else None
+
+
+def _of(t: torch.Tensor, shape, dtype, dev, name):
+    if t.dtype != dtype or t.device != dev or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _strided(t: torch.Tensor, shape, dev, name):
+    """Pointer and the (prompt, token) strides of rows [B, T, heads, hd] whose heads and dims are contiguous."""
+    if t.dtype not in _ROW_TYPES or t.device != dev or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a float32 or bfloat16 tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    B, T, heads, hd = shape
+    sb, st, sh, sd = t.stride()
+    if sd != 1 or (heads > 1 and sh != hd):
+        raise ValueError(f"{name}: heads and dims must be contiguous, got strides {t.stride()}")
+    return t.data_ptr(), sb if B > 1 else 0, st if T > 1 else 0
+
+
+def _call(dev, name, *args):
+    """The library call on the current stream of the tensors' device."""
+    fn = getattr(lib(), name)
+    if dev.index == torch.cuda.current_device():
+        rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if rc != CDSL_OK:
+        _check(rc)
+
+
+class QuantCache:
+    """The 8-bit paged cache of a batch of prompts: pool [layers, pages, heads, unit bytes] (uint8, see
+    ``QuantCache.empty``), table [prompts, pages per prompt] (int32 page ids)."""
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, head_dim: int, fmt: str):
+        if fmt not in _KVQ_FORMATS:
+            raise ValueError(f"fmt must be one of {sorted(_KVQ_FORMATS)}, got {fmt!r}")
+        if head_dim not in (32, 64, 128):
+            raise ValueError("head_dim must be 32, 64 or 128")
+        if pool.dim() != 4 or table.dim() != 2:
+            raise ValueError("pool must be [layers, pages, heads, unit], table [prompts, pages]")
+        if not pool.is_cuda:
+            raise ValueError("pool must be a device tensor")
+        layers, pages, heads, unit = pool.shape
+        if unit != 64 * head_dim + 256:
+            raise ValueError(f"a unit has 64 * head_dim + 256 = {64 * head_dim + 256} bytes, the pool {unit}")
+        self.pool, self.table, self.head_dim, self.fmt = pool, table, head_dim, fmt
+        self.batch, self.n_kv_heads, self.device = table.shape[0], heads, pool.device
+        self._c = KVQ(_of(pool, pool.shape, torch.uint8, pool.device, "pool"), _ints(table, table.shape, pool.device,
+                                                                                  "table"),
+                      layers, pages, heads, head_dim, table.shape[0], table.shape[1], _KVQ_FORMATS[fmt])
+        self._ref = C.addressof(self._c)
+
+    @staticmethod
+    def empty(layers: int, pages: int, n_kv_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
+        """A pool without contents."""
+        n = lib().cdsl_op_kvq_pool_bytes(layers, pages, n_kv_heads, head_dim)
+        if n == 0:
+            raise ValueError("pool sizes must be positive and head_dim 32, 64 or 128")
+        return torch.empty((layers, pages, n_kv_heads, n // (layers * pages * n_kv_heads)), dtype=torch.uint8,
+                           device=device)
+
+
+def cdsl_op_kvq_write(cache: QuantCache, K: torch.Tensor, V: torch.Tensor, start: Optional[torch.Tensor] = None,
+                      count: Optional[torch.Tensor] = None, layer: int = 0) -> None:
+    """K, V [B, T, heads, hd] (float32 or bfloat16; prompts and tokens may be strided) to positions start[b] + t,
+    t < count[b]."""
+    dev, B = cache.device, cache.batch
+    if K.dim() != 4:
+        raise ValueError("K must be [B, T, heads, hd]")
+    shape = (B, K.shape[1], cache.n_kv_heads, cache.head_dim)
+    if K.dtype != V.dtype:
+        raise ValueError(f"K and V must have one type, got {K.dtype} and {V.dtype}")
+    k, ksb, kst = _strided(K, shape, dev, "K")
+    v, vsb, vst = _strided(V, shape, dev, "V")
+    _call(dev, "cdsl_op_kvq_write", cache._ref, layer, k, v, _ROW_TYPES[K.dtype], shape[1], ksb, kst, vsb, vst,
+          _ints(start, (B,), dev, "start"), _ints(count, (B,), dev, "count"))
+
+
+def cdsl_op_kvq_read(cache: QuantCache, T: int, start: Optional[torch.Tensor] = None,
+                     count: Optional[torch.Tensor] = None, layer: int = 0, dtype: torch.dtype = torch.float32, out=None):
+    """(K, V) [B, T, heads, hd] of positions start[b] + t, t < count[b]; the rows behind are zeros, or stay as they are
+    in out, a (K, V) pair of contiguous tensors."""
+    dev, B = cache.device, cache.batch
+    shape = (B, T, cache.n_kv_heads, cache.head_dim)
+    if out is None:
+        if dtype not in _ROW_TYPES:
+            raise ValueError(f"dtype must be float32 or bfloat16, got {dtype}")
+        make = torch.empty if count is None else torch.zeros
+        out = (make(shape, dtype=dtype, device=dev), make(shape, dtype=dtype, device=dev))
+    K, V = out
+    if K.dtype not in _ROW_TYPES:
+        raise ValueError(f"out must be float32 or bfloat16, got {K.dtype}")
+    _call(dev, "cdsl_op_kvq_read", cache._ref, layer, _of(K, shape, K.dtype, dev, "K"), _of(V, shape, K.dtype, dev, "V"),
+          _ROW_TYPES[K.dtype], T, _ints(start, (B,), dev, "start"), _ints(count, (B,), dev, "count"))
+    return K, V
+
+
+def cdsl_op_tree_attention(cache: QuantCache, q: torch.Tensor, lens: torch.Tensor,
+                           parents: Optional[torch.Tensor] = None, n_nodes: Optional[torch.Tensor] = None,
+                           scale: Optional[float] = None, max_len: int = 0, layer: int = 0,
+                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q [B, n, H, hd] (float32 or bfloat16; prompts and nodes may be strided); returns [B, n, H, hd] of q's type.
+    parents [B, n] (None: a causal chain); scale: 1 / sqrt(hd) unless given; max_len: a bound on lens if one is known.
+    Rows of nodes from n_nodes[b] on are zeros, or stay as they are in out."""
+    dev, B, hd = cache.device, cache.batch, cache.head_dim
+    if q.dim() != 4:
+        raise ValueError("q must be [B, n, H, hd]")
+    shape = (B, q.shape[1], q.shape[2], hd)
+    n, H = shape[1], shape[2]
+    ptr, qsb, qst = _strided(q, shape, dev, "q")
+    if out is None:
+        out = (torch.empty if n_nodes is None else torch.zeros)(shape, dtype=q.dtype, device=dev)
+    need = lib().cdsl_op_tree_attention_workspace(B, n, H, cache.n_kv_heads, hd, max_len)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call(dev, "cdsl_op_tree_attention", cache._ref, layer, ptr, _ROW_TYPES[q.dtype], n, H, qsb, qst,
+          _of(lens, (B,), torch.int32, dev, "lens"), _ints(n_nodes, (B,), dev, "n_nodes"),
+          _ints(parents, (B, n), dev, "parents"), hd ** -0.5 if scale is None else scale, max_len,
+          _of(out, shape, q.dtype, dev, "out"), ws.data_ptr() if need else None, need)
+    return out
+
+
+def cdsl_op_tree_accept(target_probs: torch.Tensor, draft_probs: torch.Tensor, tokens: torch.Tensor,
+                        parents: torch.Tensor, u: torch.Tensor, v: torch.Tensor,
+                        n_nodes: Optional[torch.Tensor] = None, replace: bool = True):
+    """target_probs, draft_probs [B, n, V], tokens, parents, u [B, n], v [B]; returns (path [B, n], n_path [B],
+    next_token [B])."""
+    if target_probs.dim() != 3 or not target_probs.is_cuda:
+        raise ValueError("target_probs must be a device tensor [B, n, V]")
+    dev = target_probs.device
+    B, n, V = target_probs.shape
+    out = torch.empty(B * (n + 2), dtype=torch.int32, device=dev)
+    path, n_path, token = out[:B * n].view(B, n), out[B * n:B * n + B], out[B * n + B:]
+    _call(dev, "cdsl_op_tree_accept", _of(target_probs, (B, n, V), torch.float32, dev, "target_probs"),
+          _of(draft_probs, (B, n, V), torch.float32, dev, "draft_probs"), B, n, V,
+          _of(tokens, (B, n), torch.int32, dev, "tokens"), _of(parents, (B, n), torch.int32, dev, "parents"),
+          _ints(n_nodes, (B,), dev, "n_nodes"), _of(u, (B, n), torch.float32, dev, "u"),
+          _of(v, (B,), torch.float32, dev, "v"), 1 if replace else 0, path.data_ptr(), n_path.data_ptr(),
+          token.data_ptr())
+    return path, n_path, token
+
+
+def cdsl_op_kvq_keep(cache: QuantCache, lens: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor) -> torch.Tensor:
+    """Moves the entries of path [B, n] to the front of each tree in all layers; returns the new lengths [B]."""
+    dev, B = cache.device, cache.batch
+    if path.dim() != 2:
+        raise ValueError("path must be [B, n]")
+    new = torch.empty(B, dtype=torch.int32, device=dev)
+    _call(dev, "cdsl_op_kvq_keep", cache._ref, _of(lens, (B,), torch.int32, dev, "lens"),
+          _ints(path, (B, path.shape[1]), dev, "path"), _of(n_path, (B,), torch.int32, dev, "n_path"), path.shape[1],
+          new.data_ptr())
+    return new
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,360 @@
+// The 8-bit paged cache: rows quantised as they are written, read back, and
+// the kept path of a tree moved to the front of the tree's slots.
+//
+// One scale per (token, KV head) row x of hd values, a = max |x|:
+//   int8  s = max(a / 127, 2^-126) (rounded to fp32), code = x / s to the
+//         nearest integer, ties to even
+//   e4m3  s = the smallest power of two with a <= 448 s, at least 2^-126;
+//         code = x / s (exact) to the nearest e4m3, ties to even
+// A row that holds a NaN or an infinity has s = NaN and codes 0: it reads
+// back as NaN.  Scales stay fp32, so that a value differs from its input by
+// its code's rounding alone.
+#include "tree.h"
+
+namespace cdsl {
+
+namespace {
+
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, float (&x)[4]);
+template <>
+__device__ __forceinline__ void load4<float>(const float* p, float (&x)[4]) {
+  const f32x4 t = *(const f32x4*)p;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = t[e];
+}
+template <>
+__device__ __forceinline__ void load4<bf16>(const bf16* p, float (&x)[4]) {
+  const bf16x4 t = *(const bf16x4*)p;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = (float)t[e];
+}
+
+// Codes of four values of one row as bytes, from the row's scale s.
+template <int FMT>
+__device__ __forceinline__ unsigned encode4(const float (&x)[4], float s) {
+  if constexpr (FMT == kE4M3) {
+    // 1 / s of a power of two, exact
+    const float inv = __uint_as_float((254u << 23) - __float_as_uint(s));
+    unsigned w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, w, true);
+    return w;
+  } else {
+    // The product with an approximate 1 / s is off by less than 2^-14, so
+    // its integer is the nearest one to x / s or next to it; the signs of
+    // x - s (n +- 1/2), which one fused multiply-add gives exactly, tell.
+    const float inv = __builtin_amdgcn_rcpf(s);
+    unsigned w = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float n = __builtin_rintf(x[e] * inv);
+      const float up = fmaf(-s, n + 0.5f, x[e]), dn = fmaf(-s, n - 0.5f, x[e]);
+      const bool odd = (int)n & 1;
+      if (up > 0.f || (up == 0.f && odd)) n += 1.f;
+      else if (dn < 0.f || (dn == 0.f && odd)) n -= 1.f;
+      w |= ((unsigned)(int)n & 255u) << (8 * e);
+    }
+    return w;
+  }
+}
+
+template <int FMT>
+__device__ __forceinline__ float scale_of(float a) {
+  if constexpr (FMT == kE4M3) {
+    const unsigned u = __float_as_uint(a);
+    // a = m 2^e: 448 = 1.75 * 2^8
+    const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return __uint_as_float((unsigned)max(e, 1) << 23);
+  } else {
+    return fmaxf(a / 127.f, 1.1754943508222875e-38f);
+  }
+}
+
+template <int FMT>
+__device__ __forceinline__ void decode4(unsigned w, float s, float (&y)[4]) {
+  if constexpr (FMT == kE4M3) {
+    y[0] = __builtin_amdgcn_cvt_f32_fp8(w, 0) * s;
+    y[1] = __builtin_amdgcn_cvt_f32_fp8(w, 1) * s;
+    y[2] = __builtin_amdgcn_cvt_f32_fp8(w, 2) * s;
+    y[3] = __builtin_amdgcn_cvt_f32_fp8(w, 3) * s;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (float)(int8_t)(w >> (8 * e)) * s;
+  }
+}
+
+// Bytes (t, e) -> (e, t) of four words.
+__device__ __forceinline__ void transpose4(const unsigned (&w)[4], unsigned (&o)[4]) {
+  const unsigned a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400);
+  const unsigned c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+  o[0] = __builtin_amdgcn_perm(b, a, 0x05040100);
+  o[1] = __builtin_amdgcn_perm(b, a, 0x07060302);
+  o[2] = __builtin_amdgcn_perm(d, c, 0x05040100);
+  o[3] = __builtin_amdgcn_perm(d, c, 0x07060302);
+}
+
+// Threads of a workgroup: a task is four slots x four dims of the keys or of
+// the values (16 hd / 4 tasks a unit), so that a quarter-row load or store of
+// the fp32 or bf16 side is contiguous over the lanes and a task's 4 x 4 codes
+// are whole words in both orders.
+template <int HD>
+constexpr int kvq_threads() { return 4 * HD < 256 ? 4 * HD : 256; }
+
+// Workgroup = (page of the prompt's run, KV head, prompt).  The bytes of the
+// rows bound it (in fp32 they are 4 of every 5 bytes moved).
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(kvq_threads<HD>()) void kvq_write_kernel(KvqView c, KvqRows r) {
+  constexpr int NT = kvq_threads<HD>();
+  constexpr int LQ = HD / 4;                 // lanes per quad of slots
+  constexpr int PER = 4 * HD / NT;           // tasks per thread
+  __shared__ __attribute__((aligned(16))) unsigned lds[2 * kPage * HD / 4];
+  const int b = blockIdx.y, h = blockIdx.x % c.Hkv;
+  const KvqRun run = kvq_run(r.start, r.count, r.T, b);
+  const long long beg = run.beg, end = run.end;
+  const long long page = kvq_first_page(run) + blockIdx.x / c.Hkv;
+  const long long base = page * kPage;
+  if (base >= end || base + kPage <= beg) return;
+  uint8_t* unit = kvq_unit_of(c, b, page, h);
+  if (!unit) return;
+  const bool whole = base >= beg && base + kPage <= end;
+  float x[PER][4][4];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int task = threadIdx.x + NT * u;
+    const int isv = task / (8 * LQ), quad = task / LQ % 8, d = task % LQ * 4;
+    const T* src = (const T*)(isv ? r.V : r.K) + (isv ? r.vsb : r.ksb) * b + h * HD + d;
+    const long long ts = isv ? r.vst : r.kst;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const long long pos = base + 4 * quad + t;
+      if (pos >= beg && pos < end) load4<T>(src + (pos - beg) * ts, x[u][t]);
+      else x[u][t][0] = x[u][t][1] = x[u][t][2] = x[u][t][3] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int task = threadIdx.x + NT * u;
+    const int isv = task / (8 * LQ), quad = task / LQ % 8, d = task % LQ * 4;
+    float s[4];
+    unsigned w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      // the largest bit pattern of |x|: NaN and infinity stay on top
+      unsigned a = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a = max(a, __float_as_uint(x[u][t][e]) & 0x7fffffffu);
+#pragma unroll
+      for (int o = LQ / 2; o > 0; o >>= 1) a = max(a, (unsigned)__shfl_xor((int)a, o, 64));
+      const bool bad = a >= 0x7f800000u;
+      s[t] = bad ? __uint_as_float(0x7fc00000u) : scale_of<FMT>(__uint_as_float(a));
+      w[t] = bad ? 0u : encode4<FMT>(x[u][t], s[t]);
+    }
+    const int slot = 4 * quad;
+    float* sc = (float*)(unit + (isv ? kvq_value_scale_at(HD, slot) : kvq_key_scale_at(HD, slot)));
+    if (d == 0) {
+      if (whole) *(f32x4*)sc = (f32x4){s[0], s[1], s[2], s[3]};
+      else
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (base + slot + t >= beg && base + slot + t < end) sc[t] = s[t];
+    }
+    unsigned o[4];
+    if (isv) transpose4(w, o);
+    if (whole) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (isv) lds[kvq_value_at(HD, slot, d + t) / 4] = o[t];
+        else lds[kvq_key_at(slot + t, d) / 4] = w[t];
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bool live = base + slot + t >= beg && base + slot + t < end;
+        if (!live) continue;
+        if (!isv) *(unsigned*)(unit + kvq_key_at(slot + t, d)) = w[t];
+        else
+#pragma unroll
+          for (int e = 0; e < 4; ++e) unit[kvq_value_at(HD, slot + t, d + e)] = (uint8_t)(w[t] >> (8 * e));
+      }
+    }
+  }
+  if (!whole) return;   // uniform over the workgroup
+  __syncthreads();
+#pragma unroll
+  for (int i = threadIdx.x; i < 2 * kPage * HD / 16; i += NT) *((u32x4*)unit + i) = *((const u32x4*)lds + i);
+}
+
+// Workgroup = (page of the prompt's run, KV head, prompt): the unit comes in
+// as 16-byte pieces, the rows leave as whole lines.  Rows of a page outside
+// the pool are NaN.
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(kvq_threads<HD>()) void kvq_read_kernel(KvqView c, KvqRows r) {
+  constexpr int NT = kvq_threads<HD>();
+  constexpr int LQ = HD / 4;
+  constexpr int PER = 4 * HD / NT;
+  constexpr int WORDS = kvq_unit_bytes(HD) / 4;
+  __shared__ __attribute__((aligned(16))) unsigned lds[WORDS];
+  const int b = blockIdx.y, h = blockIdx.x % c.Hkv;
+  const KvqRun run = kvq_run(r.start, r.count, r.T, b);
+  const long long beg = run.beg, end = run.end;
+  const long long page = kvq_first_page(run) + blockIdx.x / c.Hkv;
+  const long long base = page * kPage;
+  if (base >= end || base + kPage <= beg) return;
+  const uint8_t* unit = kvq_unit_of(c, b, page, h);
+  if (unit) {
+    for (int i = threadIdx.x; i < WORDS / 4; i += NT) *((u32x4*)lds + i) = *((const u32x4*)unit + i);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int task = threadIdx.x + NT * u;
+    const int isv = task / (8 * LQ), slot = task / LQ % 8 * 4, d = task % LQ * 4;
+    unsigned w[4];
+    float s[4];
+    if (unit) {
+      unsigned o[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        o[t] = lds[(isv ? kvq_value_at(HD, slot, d + t) : kvq_key_at(slot + t, d)) / 4];
+        s[t] = __uint_as_float(lds[(isv ? kvq_value_scale_at(HD, slot + t) : kvq_key_scale_at(HD, slot + t)) / 4]);
+      }
+      if (isv) transpose4(o, w);
+      else
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w[t] = o[t];
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) w[t] = 0u, s[t] = __uint_as_float(0x7fc00000u);
+    }
+    T* dst = (T*)(isv ? r.Vo : r.Ko) + h * HD + d;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const long long pos = base + slot + t;
+      if (pos < beg || pos >= end) continue;
+      float y[4];
+      decode4<FMT>(w[t], s[t], y);
+      T* o = dst + ((long long)b * r.T + (pos - beg)) * c.Hkv * HD;
+      if constexpr (sizeof(T) == 4) *(f32x4*)o = (f32x4){y[0], y[1], y[2], y[3]};
+      else *(bf16x4*)o = (bf16x4){(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+    }
+  }
+}
+
+// One wave per (layer, KV head, prompt).  Entry i of the path moves from
+// slot L + path[i] to L + i.  Eight entries at a time are read before any of
+// them is written; with path ascending, path[i] >= i, so that no later
+// entry's source has been written by then.
+template <int HD>
+__global__ __launch_bounds__(64) void kvq_keep_kernel(KvqView c, long long layer_bytes, const int* lens,
+                                                      const int* path, const int* n_path, int n, int* new_lens) {
+  constexpr int CH = 8;
+  constexpr int KPL = (HD / 8 * CH + 63) / 64;   // 8-byte key pieces per lane
+  constexpr int VPL = (HD * CH + 63) / 64;       // value bytes per lane
+  const int b = blockIdx.y, h = blockIdx.x % c.Hkv, layer = blockIdx.x / c.Hkv;
+  const int lane = threadIdx.x;
+  c.pool += layer * layer_bytes;
+  const int L = max(lens[b], 0);
+  const int m = min(max(n_path[b], 0), n);
+  if (new_lens && blockIdx.x == 0 && lane == 0) new_lens[b] = L + m;
+  for (int i0 = 0; i0 < m; i0 += CH) {
+    // lanes 0..7: an entry's source and destination units (null: not moved)
+    const uint8_t* src = nullptr;
+    uint8_t* dst = nullptr;
+    int ss = 0, ds = 0;
+    if (lane < CH && i0 + lane < m) {
+      const int i = i0 + lane, from = path[(long long)b * n + i];
+      if (from > i && from < kTreeMax) {
+        const long long sp = (long long)L + from, dp = (long long)L + i;
+        src = kvq_unit_of(c, b, sp / kPage, h);
+        dst = kvq_unit_of(c, b, dp / kPage, h);
+        if (!src || !dst) src = dst = nullptr;
+        ss = (int)(sp % kPage);
+        ds = (int)(dp % kPage);
+      }
+    }
+    if (!__ballot(src != nullptr)) continue;
+    const uint8_t* su[CH];
+    uint8_t* du[CH];
+    int sl[CH], dl[CH];
+#pragma unroll
+    for (int u = 0; u < CH; ++u) {
+      su[u] = (const uint8_t*)__shfl((long long)src, u, 64);
+      du[u] = (uint8_t*)__shfl((long long)dst, u, 64);
+      sl[u] = __shfl(ss, u, 64);
+      dl[u] = __shfl(ds, u, 64);
+    }
+    uint2 kr[CH];
+    uint8_t vr[CH][(HD + 63) / 64];
+    unsigned sc[CH];
+#pragma unroll
+    for (int u = 0; u < CH; ++u) {
+      if (!su[u]) continue;
+      if (lane < HD / 8) kr[u] = *(const uint2*)(su[u] + kvq_key_at(sl[u], 8 * lane));
+      else if (lane < HD / 8 + 2)
+        sc[u] = *(const unsigned*)(su[u] + (lane == HD / 8 ? kvq_key_scale_at(HD, sl[u]) : kvq_value_scale_at(HD, sl[u])));
+#pragma unroll
+      for (int e = 0; e < (HD + 63) / 64; ++e)
+        if (lane + 64 * e < HD) vr[u][e] = su[u][kvq_value_at(HD, sl[u], lane + 64 * e)];
+    }
+#pragma unroll
+    for (int u = 0; u < CH; ++u) {
+      if (!su[u]) continue;
+      if (lane < HD / 8) *(uint2*)(du[u] + kvq_key_at(dl[u], 8 * lane)) = kr[u];
+      else if (lane < HD / 8 + 2)
+        *(unsigned*)(du[u] + (lane == HD / 8 ? kvq_key_scale_at(HD, dl[u]) : kvq_value_scale_at(HD, dl[u]))) = sc[u];
+#pragma unroll
+      for (int e = 0; e < (HD + 63) / 64; ++e)
+        if (lane + 64 * e < HD) du[u][kvq_value_at(HD, dl[u], lane + 64 * e)] = vr[u][e];
+    }
+  }
+}
+
+template <int HD, int FMT>
+hipError_t rows_launch(const KvqView& c, const KvqRows& r, bool write, hipStream_t st) {
+  const dim3 grid((unsigned)(kvq_run_pages(r.T) * c.Hkv), (unsigned)c.B);
+  const int nt = kvq_threads<HD>();
+  if (write) {
+    if (r.dtype == 1) kvq_write_kernel<HD, FMT, bf16><<<grid, nt, 0, st>>>(c, r);
+    else kvq_write_kernel<HD, FMT, float><<<grid, nt, 0, st>>>(c, r);
+  } else {
+    if (r.dtype == 1) kvq_read_kernel<HD, FMT, bf16><<<grid, nt, 0, st>>>(c, r);
+    else kvq_read_kernel<HD, FMT, float><<<grid, nt, 0, st>>>(c, r);
+  }
+  return hipGetLastError();
+}
+
+template <int HD>
+hipError_t rows_format(const KvqView& c, const KvqRows& r, bool write, hipStream_t st) {
+  return c.format == kE4M3 ? rows_launch<HD, kE4M3>(c, r, write, st) : rows_launch<HD, kInt8>(c, r, write, st);
+}
+
+hipError_t rows_any(const KvqView& c, const KvqRows& r, bool write, hipStream_t st) {
+  if (c.B == 0 || r.T == 0) return hipSuccess;
+  switch (c.hd) {
+    case 32: return rows_format<32>(c, r, write, st);
+    case 64: return rows_format<64>(c, r, write, st);
+    case 128: return rows_format<128>(c, r, write, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t kvq_write_launch(const KvqView& c, const KvqRows& r, hipStream_t st) { return rows_any(c, r, true, st); }
+hipError_t kvq_read_launch(const KvqView& c, const KvqRows& r, hipStream_t st) { return rows_any(c, r, false, st); }
+
+hipError_t kvq_keep_launch(const KvqView& c, int n_layers, long long layer_bytes, const int* lens, const int* path,
+                           const int* n_path, int n, int* new_lens, hipStream_t st) {
+  if (c.B == 0) return hipSuccess;
+  const dim3 grid((unsigned)(n_layers * c.Hkv), (unsigned)c.B);
+  switch (c.hd) {
+    case 32: kvq_keep_kernel<32><<<grid, 64, 0, st>>>(c, layer_bytes, lens, path, n_path, n, new_lens); break;
+    case 64: kvq_keep_kernel<64><<<grid, 64, 0, st>>>(c, layer_bytes, lens, path, n_path, n, new_lens); break;
+    case 128: kvq_keep_kernel<128><<<grid, 64, 0, st>>>(c, layer_bytes, lens, path, n_path, n, new_lens); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace cdsl

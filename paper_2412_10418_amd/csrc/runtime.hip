@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 #include <new>
 #include <string>
@@ -22,10 +23,14 @@
 #include "common.h"
 #include "gemm.h"
 #include "kernels.h"
+#include "tree.h"
 
 using namespace cdsl;
 
 static_assert(kBlock == kPoolBlock, "KV blocks and the pool bookkeeping agree on the block size");
+static_assert(kPage == CDSL_KVQ_PAGE && kTreeMax == CDSL_TREE_MAX && kAcceptMaxVocab == CDSL_ACCEPT_MAX_VOCAB &&
+                  kInt8 == CDSL_KVQ_INT8 && kE4M3 == CDSL_KVQ_E4M3,
+              "the kernels' limits are those of the header");
 
 namespace {
 
@@ -1867,3 +1872,167 @@ int cdsl_op_lm_head_rows(const float* A, const void* B, int32_t M, int32_t V, in
   return CDSL_OK;
 }
 
+// ---------------------------------------------------------------------------
+// a drafted tree served from an 8-bit paged cache (include/cdsl_ops.h)
+// ---------------------------------------------------------------------------
+namespace {
+
+// workgroups of one grid dimension: a launch's threads (256 each) stay below 2^32
+constexpr long long kMaxGroups = (1 << 24) - 1;
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// one of the strides (in elements) that must keep rows 16-byte aligned
+bool aligned_stride(int64_t s, int32_t dtype) { return s * (dtype == CDSL_BF16 ? 2 : 4) % 16 == 0; }
+
+// CDSL_OK, or the error of a cache descriptor
+int kvq_check(const cdsl_kvq* c) {
+  if (!c || !c->pool || (!c->table && c->batch != 0))
+    return fail(nullptr, CDSL_EINVAL, "null cache, pool or table");
+  if (c->n_layers <= 0 || c->pages <= 0 || c->n_kv_heads <= 0 || c->batch < 0 || c->table_stride <= 0)
+    return fail(nullptr, CDSL_EINVAL, "bad cache sizes");
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128)
+    return fail(nullptr, CDSL_EINVAL, "head_dim must be 32, 64 or 128");
+  if (c->format != CDSL_KVQ_INT8 && c->format != CDSL_KVQ_E4M3) return fail(nullptr, CDSL_EINVAL, "bad cache format");
+  if (!aligned16(c->pool)) return fail(nullptr, CDSL_EINVAL, "the pool must be 16-byte aligned");
+  if (c->batch > 65535) return fail(nullptr, CDSL_ERANGE, "more than 65535 prompts");
+  return CDSL_OK;
+}
+
+long long kvq_layer_bytes(const cdsl_kvq* c) {
+  return (long long)c->pages * c->n_kv_heads * kvq_unit_bytes(c->head_dim);
+}
+
+KvqView kvq_view(const cdsl_kvq* c, int32_t layer) {
+  return KvqView{(uint8_t*)c->pool + layer * kvq_layer_bytes(c), c->table, c->batch, c->table_stride, c->pages,
+                 c->n_kv_heads, c->head_dim, c->format};
+}
+
+int kvq_rows_check(const cdsl_kvq* c, int32_t layer, const void* K, const void* V, int32_t dtype, int32_t T) {
+  const int rc = kvq_check(c);
+  if (rc != CDSL_OK) return rc;
+  if (layer < 0 || layer >= c->n_layers) return fail(nullptr, CDSL_EINVAL, "bad layer");
+  if (dtype != CDSL_F32 && dtype != CDSL_BF16) return fail(nullptr, CDSL_EINVAL, "bad dtype");
+  if (T < 0) return fail(nullptr, CDSL_EINVAL, "bad row count");
+  if ((!K || !V) && T != 0 && c->batch != 0) return fail(nullptr, CDSL_EINVAL, "null rows");
+  if (!aligned16(K) || !aligned16(V)) return fail(nullptr, CDSL_EINVAL, "rows must be 16-byte aligned");
+  if ((T / kPage + 2LL) * c->n_kv_heads > kMaxGroups) return fail(nullptr, CDSL_ERANGE, "too many rows");
+  return CDSL_OK;
+}
+
+int launched(hipError_t e) {
+  return e == hipSuccess ? CDSL_OK : fail(nullptr, CDSL_EDEVICE, hipGetErrorString(e));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cdsl_op_kvq_pool_bytes(int32_t n_layers, int32_t pages, int32_t n_kv_heads, int32_t head_dim) {
+  if (n_layers <= 0 || pages <= 0 || n_kv_heads <= 0 || (head_dim != 32 && head_dim != 64 && head_dim != 128)) return 0;
+  return (size_t)n_layers * pages * n_kv_heads * kvq_unit_bytes(head_dim);
+}
+
+int cdsl_op_kvq_write(const cdsl_kvq* cache, int32_t layer, const void* K, const void* V, int32_t dtype, int32_t T,
+                      int64_t k_stride_b, int64_t k_stride_t, int64_t v_stride_b, int64_t v_stride_t,
+                      const int32_t* start, const int32_t* count, void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    const int rc = kvq_rows_check(cache, layer, K, V, dtype, T);
+    if (rc != CDSL_OK) return rc;
+    for (int64_t s : {k_stride_b, k_stride_t, v_stride_b, v_stride_t})
+      if (!aligned_stride(s, dtype)) return fail(nullptr, CDSL_EINVAL, "row strides must be multiples of 16 bytes");
+    const KvqRows r{K, V, nullptr, nullptr, dtype, T, k_stride_b, k_stride_t, v_stride_b, v_stride_t, start, count};
+    return launched(kvq_write_launch(kvq_view(cache, layer), r, (hipStream_t)stream));
+  });
+}
+
+int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V, int32_t dtype, int32_t T,
+                     const int32_t* start, const int32_t* count, void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    const int rc = kvq_rows_check(cache, layer, K, V, dtype, T);
+    if (rc != CDSL_OK) return rc;
+    const KvqRows r{nullptr, nullptr, K, V, dtype, T, 0, 0, 0, 0, start, count};
+    return launched(kvq_read_launch(kvq_view(cache, layer), r, (hipStream_t)stream));
+  });
+}
+
+size_t cdsl_op_tree_attention_workspace(int32_t batch, int32_t n, int32_t H, int32_t n_kv_heads, int32_t head_dim,
+                                        int32_t max_len) {
+  if (batch <= 0 || n <= 0 || H <= 0 || n_kv_heads <= 0 || H % n_kv_heads != 0 || (long long)n * H > (1 << 30)) return 0;
+  return tree_attn_plan(batch, n, H, n_kv_heads, head_dim, std::max(max_len, 0)).workspace;
+}
+
+int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, int32_t dtype, int32_t n, int32_t H,
+                           int64_t q_stride_b, int64_t q_stride_t, const int32_t* lens, const int32_t* n_nodes,
+                           const int32_t* parents, float scale, int32_t max_len, void* out, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    const int rc = kvq_check(cache);
+    if (rc != CDSL_OK) return rc;
+    if (layer < 0 || layer >= cache->n_layers) return fail(nullptr, CDSL_EINVAL, "bad layer");
+    if ((!Q || !lens || !out) && n != 0 && cache->batch != 0) return fail(nullptr, CDSL_EINVAL, "null argument");
+    if (dtype != CDSL_F32 && dtype != CDSL_BF16) return fail(nullptr, CDSL_EINVAL, "bad dtype");
+    if (n < 0 || H <= 0 || H % cache->n_kv_heads != 0) return fail(nullptr, CDSL_EINVAL, "bad node or head count");
+    if (!std::isfinite(scale)) return fail(nullptr, CDSL_EINVAL, "scale must be finite");
+    if (!aligned16(Q) || !aligned16(out) || !aligned16(workspace))
+      return fail(nullptr, CDSL_EINVAL, "Q, out and workspace must be 16-byte aligned");
+    if (!aligned_stride(q_stride_b, dtype) || !aligned_stride(q_stride_t, dtype))
+      return fail(nullptr, CDSL_EINVAL, "row strides must be multiples of 16 bytes");
+    if (parents && n > CDSL_TREE_MAX) return fail(nullptr, CDSL_ERANGE, "a tree has at most 512 nodes");
+    if ((long long)n * H > (1 << 30)) return fail(nullptr, CDSL_ERANGE, "n * H exceeds 2^30");
+    if (cache->batch == 0 || n == 0) return CDSL_OK;
+    const TreeAttnPlan p = tree_attn_plan(cache->batch, n, H, cache->n_kv_heads, cache->head_dim, std::max(max_len, 0));
+    if ((long long)p.row_groups * p.nsplit * cache->batch * cache->n_kv_heads > kMaxGroups ||
+        (long long)cache->batch * n * H > kMaxGroups)
+      return fail(nullptr, CDSL_ERANGE, "too many rows");
+    if (p.workspace > 0 && (!workspace || workspace_bytes < p.workspace))
+      return fail(nullptr, CDSL_EINVAL, "workspace too small");
+    TreeAttnArgs a{};
+    a.c = kvq_view(cache, layer);
+    a.q = Q;
+    a.qsb = q_stride_b;
+    a.qst = q_stride_t;
+    a.out = out;
+    a.lens = lens;
+    a.n_nodes = n_nodes;
+    a.parents = parents;
+    a.n = n;
+    a.H = H;
+    a.G = H / cache->n_kv_heads;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    return launched(tree_attn_launch(a, p, dtype, workspace, (hipStream_t)stream));
+  });
+}
+
+int cdsl_op_tree_accept(const float* target_probs, const float* draft_probs, int32_t batch, int32_t n, int32_t V,
+                        const int32_t* tokens, const int32_t* parents, const int32_t* n_nodes, const float* u,
+                        const float* v, int32_t replace, int32_t* path, int32_t* n_path, int32_t* next_token,
+                        void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    if ((!target_probs || !draft_probs || !tokens || !parents || !u || !v || !path || !n_path || !next_token) &&
+        batch != 0)
+      return fail(nullptr, CDSL_EINVAL, "null argument");
+    if (batch < 0 || n <= 0 || V <= 0) return fail(nullptr, CDSL_EINVAL, "bad sizes");
+    if (n > CDSL_TREE_MAX) return fail(nullptr, CDSL_ERANGE, "a tree has at most 512 nodes");
+    if (V > CDSL_ACCEPT_MAX_VOCAB) return fail(nullptr, CDSL_ERANGE, "vocabulary beyond 2^20");
+    return launched(tree_accept_launch(target_probs, draft_probs, batch, n, V, tokens, parents, n_nodes, u, v,
+                                       replace, path, n_path, next_token, (hipStream_t)stream));
+  });
+}
+
+int cdsl_op_kvq_keep(const cdsl_kvq* cache, const int32_t* lens, const int32_t* path, const int32_t* n_path, int32_t n,
+                     int32_t* new_lens, void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    const int rc = kvq_check(cache);
+    if (rc != CDSL_OK) return rc;
+    if ((!lens || !n_path || (!path && n != 0)) && cache->batch != 0)
+      return fail(nullptr, CDSL_EINVAL, "null argument");
+    if (n < 0) return fail(nullptr, CDSL_EINVAL, "bad node count");
+    if (new_lens && new_lens == lens) return fail(nullptr, CDSL_EINVAL, "new_lens must not be lens");
+    if ((long long)cache->n_layers * cache->n_kv_heads > kMaxGroups) return fail(nullptr, CDSL_ERANGE, "too many heads");
+    return launched(kvq_keep_launch(kvq_view(cache, 0), cache->n_layers, kvq_layer_bytes(cache), lens, path, n_path, n,
+                                    new_lens, (hipStream_t)stream));
+  });
+}
+
+}  // extern "C"
