@@ -67,16 +67,17 @@ CDSL_KVQ_HD long long kvq_first_page(const KvqRun& r) { return (r.beg >= 0 ? r.b
 CDSL_KVQ_HD int kvq_run_pages(int T) { return T / kPage + (T % kPage ? 1 : 0) + 1; }
 
 // Bit s of the result: whether slot s of a page is visible to a node.  i0 =
-// page * 32 - L > -32 is the node in the page's slot 0 (negative: so many
-// prompt tokens come first).  Chain: the nodes up to `node`.  Tree: the nodes
+// page * 32 - L is the node in the page's slot 0 (negative: so many prompt
+// tokens come first).  Chain: the nodes up to `node`.  Tree: the nodes
 // whose bit is set in `mask`, kTreeMax bits and a word of zeros behind.
 constexpr int kTreeMax = 512;            // nodes of a tree with parents
 constexpr int kTreeWords = kTreeMax / 32 + 1;
 CDSL_KVQ_HD uint32_t slots_of_chain(int i0, int node) {
-  const int last = node - i0;
+  const int last = node - i0;   // the node's slot
   return last >= 31 ? ~0u : last < 0 ? 0u : (2u << last) - 1u;
 }
 CDSL_KVQ_HD uint32_t slots_of_tree(int i0, const uint32_t* mask) {
+  if (i0 <= -kPage) return ~0u;
   if (i0 < 0) return (mask[0] << -i0) | ((1u << -i0) - 1u);
   const uint64_t w = (uint64_t)mask[(i0 >> 5) + 1] << 32 | mask[i0 >> 5];
   return (uint32_t)(w >> (i0 & 31));

@@ -1,4 +1,4 @@
-// Attention of a token tree over the 8-bit paged cache: the kernel, one
+// Attention of a token tree over the 8-bit paged cache: the kernels, one
 // instance file per head dimension (tree_attention_*.hip).
 //
 //   o_i = sum_j softmax_j(scale q_i . k_j) v_j
@@ -7,46 +7,53 @@
 // With k = s_k c_k and v = s_v c_v (codes c, one scale per token and KV head)
 // the scales leave the sums over dims: s_k multiplies a score, s_v a
 // probability, and the matrix products run on the codes, which are exact in
-// bf16.  One pass over the keys with a running maximum and sum (fp32).
-//
-// Workgroup = (key split, prompt x KV head, group of 16-row tiles); the rows
-// of a (prompt, KV head) are its nodes x the G query heads of that KV head.
-// Its four waves are row groups x KW key groups; a wave takes RPW row tiles
-// and every KW-th page, whose codes go from memory straight to its registers:
-// the cache holds them in operand order (tree.h), so there is no LDS stage
-// and no barrier in the loop.  Scores are computed transposed,
+// f16 and in bf16.  One pass over the keys with a running maximum and sum
+// (fp32).  The rows of a (prompt, KV head) are its nodes x the G query heads
+// of that KV head, in tiles of 16.  Scores are computed transposed,
 //   S^T[16 keys, 16 rows] = K[16, hd] . Q^T[hd, 16]       (MFMA 16x16x32)
 // so that a lane's scores are its operand of the second product,
 //   O^T[16 dims, 16 rows] += V^T[16 dims, 32 keys] . P^T[32 keys, 16 rows].
-// Key groups merge through LDS, key splits through a second kernel, both in
-// a fixed order.
+//
+// Precision.  A row of q is scaled by a power of two to a largest entry in
+// [1, 2) and taken as f16 planes: two for fp32 activations (24 bits of the
+// largest entry), one for bf16 (exact down to 2^-17 of the largest entry).
+// Probabilities times s_v can be of any size, so they stay bf16: three planes
+// (their 24 bits) for fp32, one (2^-8 of each, independent over the keys; the
+// result rounds by as much) for bf16.  Two planes would lose 2^-16 of each
+// probability: 2.5e-6 of the result, where fp32 products give 0.8e-6.
+//
+// Two kernels.  Few rows (one or two tiles): the codes go from memory
+// straight to the registers of the wave that uses them, and the waves of a
+// workgroup take different pages (tree_few_kernel).  More rows: the
+// workgroup's waves take different rows, and the pages are converted once for
+// all of them through LDS (tree_many_kernel).
 #pragma once
+#include <type_traits>
+
 #include "tree.h"
 
 namespace cdsl {
 
 namespace {
 
-// Eight codes (two words, slots or dims in order) as bf16, exact.
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
+
+constexpr float kLazy = 8.f;   // log2 units that the running maximum may lag behind
+
+// Eight codes (two words) as bf16, exact.
 template <int FMT>
-__device__ __forceinline__ bf16x8 codes8(unsigned a, unsigned b) {
+__device__ __forceinline__ bf16x8 codes_bf16(unsigned a, unsigned b) {
   union {
     unsigned u[4];
+    bf16x2v p[4];
     bf16x8 v;
   } o;
   if constexpr (FMT == kE4M3) {
-    union {
-      bf16x2v v;
-      unsigned u;
-    } t;
-    t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false);
-    o.u[0] = t.u;
-    t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
-    o.u[1] = t.u;
-    t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false);
-    o.u[2] = t.u;
-    t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
-    o.u[3] = t.u;
+    o.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false);
+    o.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
+    o.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false);
+    o.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
   } else {
     // an 8-bit integer has at most 7 significant bits: the upper half of
     // its fp32 form is its bf16 form
@@ -62,8 +69,32 @@ __device__ __forceinline__ bf16x8 codes8(unsigned a, unsigned b) {
   return o.v;
 }
 
-__device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+// Eight codes as f16, exact.
+template <int FMT>
+__device__ __forceinline__ f16x8 codes_f16(unsigned a, unsigned b) {
+  union {
+    unsigned u[4];
+    f16x2 p[4];
+    f16x8 v;
+  } o;
+  if constexpr (FMT == kE4M3) {
+    o.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false);
+    o.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
+    o.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false);
+    o.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
+  } else {
+    // 0x6400 + x is 1024 + x in f16: with x = code + 128, one subtraction
+    const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned w = (i ? b : a) ^ 0x80808080u;
+      o.u[2 * i] = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400);
+      o.u[2 * i + 1] = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402);
+      o.p[2 * i] -= off;
+      o.p[2 * i + 1] -= off;
+    }
+  }
+  return o.v;
 }
 
 // Bytes of word bits 0..3 of m as a mask.
@@ -71,143 +102,333 @@ __device__ __forceinline__ unsigned byte_mask(unsigned m) {
   return ((m & 1u) | (m & 2u) << 7 | (m & 4u) << 14 | (m & 8u) << 21) * 255u;
 }
 
-// QT float: activations in fp32.  q and p s_v are taken as three bf16 planes
-// each (their 24 bits): with two, 2^-16 of each probability is lost, and the
-// result's error is 2.5e-6 of it where fp32 products and sums give 0.8e-6.
-// QT bf16: q as it is and p s_v in bf16 (2^-8 of each probability,
-// independent over the keys; the result rounds by as much).
-template <int HD, int FMT, typename QT, int RPW, int KW>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void tree_attn_kernel(TreeAttnArgs a) {
-  constexpr int NW = 4, RTW = NW / KW;
-  constexpr int S = HD / 32, DT = HD / 16;
-  constexpr int QP = sizeof(QT) == 4 ? 3 : 1, PP = QP;   // planes of q and of p s_v
-  constexpr int ROWS = 16 * RPW * RTW;       // rows per workgroup
-  constexpr int MW = kTreeWords;             // mask words per node
-  constexpr int UNIT = kvq_unit_bytes(HD);
-  constexpr float kLazy = 8.f;
-  constexpr int SLOT = (2 + 4 * DT) * 64;    // floats a wave hands over per row tile
-  constexpr int XF = (KW - 1) * RTW * RPW * SLOT, MF = ROWS * MW + kTreeMax;
-  __shared__ float lds[XF > MF ? XF : MF];
+// e4m3 codes of slots past the last node (never written) may be NaNs: zeros.
+__device__ __forceinline__ u32x4 hold_values(u32x4 w, int held, int lg) {
+  const unsigned hm = held >= 32 ? ~0u : (1u << held) - 1u;
+  const unsigned mA = byte_mask(hm >> (4 * lg)), mB = byte_mask(hm >> (16 + 4 * lg));
+  return (u32x4){w.x & mA, w.y & mB, w.z & mA, w.w & mB};
+}
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int lr = lane & 15, lg = lane >> 4;
+// The prompt, KV head, keys and rows of a workgroup that takes `tiles` row
+// tiles of a (prompt, KV head).
+struct TreeSpan {
+  int b, kvh, split, nrows, row0, L, nb, node0, node1, beg, end;
+  bool over, none;
+};
+
+__device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs& a, int tiles) {
+  TreeSpan t;
   // The row groups of one (prompt, KV head, split) read the same pages:
   // workgroup w runs on XCD w % 8, so they take consecutive slots of one XCD.
   const int NR = a.row_groups, NC = gridDim.x / NR, full = NC & ~7;
   int chunk, rg;
   if ((int)blockIdx.x < full * NR) {
-    const int t = blockIdx.x >> 3;
-    chunk = (blockIdx.x & 7) + 8 * (t / NR);
-    rg = t % NR;
+    const int x = blockIdx.x >> 3;
+    chunk = (blockIdx.x & 7) + 8 * (x / NR);
+    rg = x % NR;
   } else {
-    const int t = blockIdx.x - full * NR;
-    chunk = full + t / NR;
-    rg = t % NR;
+    const int x = blockIdx.x - full * NR;
+    chunk = full + x / NR;
+    rg = x % NR;
   }
-  const int split = chunk % a.nsplit, pair = chunk / a.nsplit;
-  const int b = pair / a.c.Hkv, kvh = pair % a.c.Hkv;
-  const int G = a.G;
-  const int nb = a.n_nodes ? min(max(a.n_nodes[b], 0), a.n) : a.n;
-  const int nrows = nb * G, row0 = rg * ROWS;
-  if (row0 >= nrows) return;   // uniform over the workgroup
-  const int L = max(a.lens[b], 0);
-  const int node0 = row0 / G, node1 = (min(row0 + ROWS, nrows) - 1) / G;
+  t.split = chunk % a.nsplit;
+  const int pair = chunk / a.nsplit;
+  t.b = pair / a.c.Hkv;
+  t.kvh = pair % a.c.Hkv;
+  t.nb = a.n_nodes ? min(max(a.n_nodes[t.b], 0), a.n) : a.n;
+  t.nrows = t.nb * a.G;
+  t.row0 = rg * 16 * tiles;
+  t.none = t.row0 >= t.nrows;
+  t.L = max(a.lens[t.b], 0);
+  t.node0 = t.row0 / a.G;
+  t.node1 = (min(t.row0 + 16 * tiles, t.nrows) - 1) / a.G;
   // a prompt that its table cannot hold has no answer: NaN, and no page read
-  const bool over = (long long)L + nb > (long long)a.c.table_stride * kPage;
-  const int pages = over ? 0 : (L + nb + kPage - 1) / kPage;
+  t.over = (long long)t.L + t.nb > (long long)a.c.table_stride * kPage;
+  const int pages = t.over ? 0 : (t.L + t.nb + kPage - 1) / kPage;
   const int per = (pages + a.nsplit - 1) / a.nsplit;
-  const int beg = split * per;
-  const int end = over ? 0 : min(min(beg + per, pages), (L + node1) / kPage + 1);
+  t.beg = t.split * per;
+  t.end = t.over ? 0 : min(min(t.beg + per, pages), (t.L + t.node1) / kPage + 1);
+  return t;
+}
 
-  const int rt = wave / KW, kw = wave % KW;
-  const int rw0 = row0 + rt * 16 * RPW;
-  const bool has_rows = rw0 < nrows;
-  int node[RPW], qrow[RPW];
-  bool valid[RPW];
+// Which nodes a node sees, for the nodes of a workgroup: masks[m - node0].  A
+// parent outside [0, own index) ends the walk, so every walk ends.
+__device__ __forceinline__ void tree_masks(const TreeAttnArgs& a, const TreeSpan& t, uint32_t* masks, int* par, int NT) {
+  const int nodes = t.node1 - t.node0 + 1;
+  for (int i = threadIdx.x; i <= t.node1; i += NT) par[i] = a.parents[(long long)t.b * a.n + i];
+  for (int i = threadIdx.x; i < nodes * kTreeWords; i += NT) masks[i] = 0u;
+  __syncthreads();
+  for (int i = threadIdx.x; i < nodes; i += NT) {
+    int m = t.node0 + i;
+    while (true) {
+      masks[i * kTreeWords + (m >> 5)] |= 1u << (m & 31);
+      const int up = par[m];
+      if (up < 0 || up >= m) break;
+      m = up;
+    }
+  }
+  __syncthreads();
+}
+
+// Over the four lanes of a row (xor 16 and 32).
+__device__ __forceinline__ float groups_max(float v) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
+  t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
+}
+
+// One tile of 16 rows in a wave: lane (row lr = lane % 16, group lg = lane / 16).
+template <int HD, typename QT>
+struct RowTile {
+  static constexpr int S = HD / 32, DT = HD / 16;
+  static constexpr int QP = sizeof(QT) == 4 ? 2 : 1;   // planes of q
+  static constexpr int PP = sizeof(QT) == 4 ? 3 : 1;   // planes of p s_v
+  f16x8 q[S][QP];
+  float rm;              // what a score of the scaled q counts in log2 units
+  f32x4 acc[DT];         // dims 16 t + 4 lg .. +3 of row lr
+  float m, l;            // running maximum (log2 units) and this lane's part of the sum
+  int node, head;
+  bool valid;
+
+  __device__ __forceinline__ void init(const TreeAttnArgs& a, const TreeSpan& t, int row, int lg) {
+    valid = row < t.nrows;
+    const int r = valid ? row : t.nrows - 1;
+    node = r / a.G;
+    head = t.kvh * a.G + r % a.G;
+    const QT* qp = (const QT*)a.q + t.b * a.qsb + node * a.qst + (long long)head * HD + 8 * lg;
+    float x[S][8];
+    unsigned top = 0;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if constexpr (sizeof(QT) == 2) {
+        const bf16x8 v = *(const bf16x8*)(qp + 32 * s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[s][e] = (float)v[e];
+      } else {
+        const f32x4 v0 = *(const f32x4*)(qp + 32 * s), v1 = *(const f32x4*)(qp + 32 * s + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[s][e] = e < 4 ? v0[e & 3] : v1[e & 3];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[s][e]) & 0x7fffffffu);
+    }
+    top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
+    top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
+    // 2^e <= max|q| < 2^(e+1); rows of zeros and the smallest numbers as 2^-126,
+    // a NaN or an infinity stays one (its scores are NaN)
+    const int e = max((int)(top >> 23), 1) - 127;
+    const float down = __builtin_ldexpf(a.scale_log2 < 0.f ? -1.f : a.scale_log2 > 0.f ? 1.f : 0.f, -e);
+    rm = a.scale_log2 == 0.f ? 1.f : __builtin_ldexpf(fabsf(a.scale_log2), e);
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        // (2^-127 and 2^-128 are subnormal, which products keep)
+        const float y = x[s][k] * down;
+        const _Float16 hi = (_Float16)y;
+        q[s][0][k] = hi;
+        if constexpr (QP > 1) q[s][1][k] = (_Float16)(y - (float)hi);
+      }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = t.over ? __uint_as_float(0x7fc00000u) : 0.f;
+  }
+
+  // What is not visible of a page: vis has this lane's slots at bits 0..3 and
+  // 16..19.  (The scales of a hidden slot may be anything.)
+  static __device__ __forceinline__ void hide(float (&s)[8], float (&vs)[8], unsigned vis) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool seen = vis >> (e < 4 ? e : 12 + e) & 1u;
+      s[e] = seen ? s[e] : -INFINITY;
+      vs[e] = seen ? vs[e] : 0.f;
+    }
+  }
+
+  // Probabilities of a page as planes of p s_v, from its scores times s_k
+  // (slots 4 lg + e and 16 + 4 lg + e).
+  __device__ __forceinline__ void softmax(const float (&s)[8], const float (&vs)[8], bf16x8 (&pf)[PP]) {
+    float mt = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+    mt = groups_max(mt) * rm;
+    // The exponentials use a maximum that may lie up to kLazy below the true
+    // one, so O is rescaled rarely; O / l does not depend on it.
+    const bool raise = mt > m + kLazy;   // true for the first visible key
+    if (__ballot(raise)) {
+      const float to = raise ? mt : m;
+      const float corr = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      l *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[d] *= corr;
+      m = to;
+    }
+    const float mu = m == -INFINITY ? 0.f : m;
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[e], rm, -mu));
+      l += p;
+      w[e] = p * vs[e];
+    }
+    if constexpr (PP == 1) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pf[0][e] = (bf16)w[e];
+    } else {
+      // planes by truncation: 8 bits each, and each rest is exact
+      union {
+        unsigned u[4];
+        bf16x8 v;
+      } o;
+#pragma unroll
+      for (int pl = 0; pl < PP; ++pl) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o.u[e] = __builtin_amdgcn_perm(__float_as_uint(w[2 * e + 1]), __float_as_uint(w[2 * e]), 0x07060302);
+        pf[pl] = o.v;
+        if (pl + 1 < PP)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] -= __uint_as_float(__float_as_uint(w[e]) & 0xffff0000u);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void finish() {
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+  }
+
+  // The result, or this split's part of it.
+  __device__ __forceinline__ void store(const TreeAttnArgs& a, const TreeSpan& t, int lg) {
+    if (!valid) return;
+    const long long row = ((long long)t.b * a.n + node) * a.H + head;
+    if (a.nsplit == 1) {
+      const float inv = 1.f / l;
+      QT* o = (QT*)a.out + row * HD + 4 * lg;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const f32x4 y = acc[d] * inv;
+        if constexpr (sizeof(QT) == 4) *(f32x4*)(o + 16 * d) = y;
+        else *(bf16x4*)(o + 16 * d) = (bf16x4){(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+      }
+    } else {
+      const long long prow = (long long)t.split * a.c.B * a.n * a.H + row;
+      float* po = a.part_o + prow * HD + 4 * lg;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) *(f32x4*)(po + 16 * d) = acc[d];
+      if (lg == 0) {
+        a.part_ml[prow * 2] = m;
+        a.part_ml[prow * 2 + 1] = l;
+      }
+    }
+  }
+};
+
+// Scores of a page's two halves; dim step s, key codes k0 and k1.  Every
+// other product belongs to another sum, so that none waits for the one before.
+template <int HD, typename QT, int RPW>
+__device__ __forceinline__ void score_step(const RowTile<HD, QT> (&row)[RPW], int s, const f16x8& k0, const f16x8& k1,
+                                           f32x4 (&sc)[RPW][2]) {
+#pragma unroll
+  for (int pl = 0; pl < RowTile<HD, QT>::QP; ++pl)
+#pragma unroll
+    for (int r = 0; r < RPW; ++r) {
+      sc[r][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, row[r].q[s][pl], sc[r][0], 0, 0, 0);
+      sc[r][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, row[r].q[s][pl], sc[r][1], 0, 0, 0);
+    }
+}
+
+// O of the dim tiles d and d + 1, value codes v0 and v1.
+template <int HD, typename QT, int RPW>
+__device__ __forceinline__ void value_step(RowTile<HD, QT> (&row)[RPW], int d, const bf16x8& v0, const bf16x8& v1,
+                                           const bf16x8 (&pf)[RPW][RowTile<HD, QT>::PP]) {
+#pragma unroll
+  for (int pl = 0; pl < RowTile<HD, QT>::PP; ++pl)
+#pragma unroll
+    for (int r = 0; r < RPW; ++r) {
+      row[r].acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[r][pl], row[r].acc[d], 0, 0, 0);
+      row[r].acc[d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[r][pl], row[r].acc[d + 1], 0, 0, 0);
+    }
+}
+
+// Planes of p s_v of every row tile of a wave, from a page's scores.
+// MASKED: the page holds nodes.
+template <bool MASKED, int HD, typename QT, int RPW>
+__device__ __forceinline__ void page_softmax(RowTile<HD, QT> (&row)[RPW], const f32x4 (&sc)[RPW][2], const f32x4 (&ks)[2],
+                                             const f32x4 (&vs)[2], bool tree, int i0, int node0,
+                                             const uint32_t* masks, int lg,
+                                             bf16x8 (&pf)[RPW][RowTile<HD, QT>::PP]) {
 #pragma unroll
   for (int r = 0; r < RPW; ++r) {
-    const int row = rw0 + 16 * r + lr;
-    valid[r] = row < nrows;
-    const int rr = valid[r] ? row : nrows - 1;
-    node[r] = rr / G;
-    qrow[r] = kvh * G + rr % G;
+    float s[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s[e] = sc[r][e >> 2][e & 3] * ks[e >> 2][e & 3];
+      v[e] = vs[e >> 2][e & 3];
+    }
+    if constexpr (MASKED) {
+      const unsigned vis = tree ? slots_of_tree(i0, masks + (row[r].node - node0) * kTreeWords)
+                                : slots_of_chain(i0, row[r].node);
+      RowTile<HD, QT>::hide(s, v, vis >> (4 * lg));
+    }
+    row[r].softmax(s, v, pf[r]);
   }
+}
+
+// Workgroup = (key split, prompt x KV head, group of RPW row tiles); its four
+// waves take every fourth page each.  No LDS stage and no barrier in the
+// loop: the cache holds the codes in operand order (kvq_layout.h), 16 bytes a
+// lane, and the next page's loads are in flight while one is computed.  The
+// waves merge through LDS, key splits through a second kernel, both in a
+// fixed order.
+template <int HD, int FMT, typename QT, int RPW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void tree_few_kernel(TreeAttnArgs a) {
+  constexpr int KW = 4;
+  using Row = RowTile<HD, QT>;
+  constexpr int S = Row::S, DT = Row::DT;
+  constexpr int UNIT = kvq_unit_bytes(HD);
+  constexpr int SLOT = (2 + 4 * DT) * 64;    // floats a wave hands over per row tile
+  constexpr int XF = (KW - 1) * RPW * SLOT, MF = 16 * RPW * kTreeWords + kTreeMax;
+  __shared__ float lds[XF > MF ? XF : MF];
+
+  const int lane = threadIdx.x & 63, kw = threadIdx.x >> 6;
+  const int lr = lane & 15, lg = lane >> 4;
+  const TreeSpan t = tree_span(a, RPW);
+  if (t.none) return;   // uniform over the workgroup
 
   // page ids of this wave's next 64 pages, one a lane
   int ids = 0;
-  const int* table = a.c.table + (long long)b * a.c.table_stride;
+  const int* table = a.c.table + (long long)t.b * a.c.table_stride;
   auto fetch_ids = [&](int it) __attribute__((always_inline)) {
-    const int p = beg + kw + KW * (it + lane);
-    ids = p < end ? table[p] : 0;
+    const int p = t.beg + kw + KW * (it + lane);
+    ids = p < t.end ? table[p] : 0;
   };
-  const int npages = has_rows && end > beg + kw ? (end - beg - kw + KW - 1) / KW : 0;
+  const int npages = t.end > t.beg + kw ? (t.end - t.beg - kw + KW - 1) / KW : 0;
   if (npages > 0) fetch_ids(0);
 
-  // Q^T fragments: row lr, dims 32 s + 8 lg .. +7
-  bf16x8 qf[RPW][S][QP];
+  Row row[RPW];
 #pragma unroll
-  for (int r = 0; r < RPW; ++r) {
-    const QT* qp = (const QT*)a.q + b * a.qsb + node[r] * a.qst + (long long)qrow[r] * HD + 8 * lg;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      if constexpr (QP == 1) {
-        qf[r][s][0] = *(const bf16x8*)(qp + 32 * s);
-      } else {
-        const f32x4 x0 = *(const f32x4*)(qp + 32 * s), x1 = *(const f32x4*)(qp + 32 * s + 4);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float x = e < 4 ? x0[e & 3] : x1[e & 3];
-#pragma unroll
-          for (int pl = 0; pl < QP; ++pl) {
-            const bf16 hi = (bf16)x;
-            qf[r][s][pl][e] = hi;
-            x -= (float)hi;
-          }
-        }
-      }
-    }
-  }
+  for (int r = 0; r < RPW; ++r) row[r].init(a, t, t.row0 + 16 * r + lr, lg);
 
-  // Which nodes a node sees: bit m of its mask.  A parent outside [0, own
-  // index) ends the walk, so every walk ends.
   const bool tree = a.parents != nullptr && a.n > 1;
-  unsigned* masks = (unsigned*)lds;
-  if (tree) {
-    int* par = (int*)lds + ROWS * MW;
-    for (int i = threadIdx.x; i <= node1; i += 256) par[i] = a.parents[(long long)b * a.n + i];
-    for (int i = threadIdx.x; i < ROWS * MW; i += 256) masks[i] = 0u;
-    __syncthreads();
-    const int i = threadIdx.x;
-    if (i <= node1 - node0) {
-      int m = node0 + i;
-      while (true) {
-        masks[i * MW + (m >> 5)] |= 1u << (m & 31);
-        const int up = par[m];
-        if (up < 0 || up >= m) break;
-        m = up;
-      }
-    }
-    __syncthreads();
-  }
-  auto visible = [&](int page, int m) __attribute__((always_inline)) -> unsigned {
-    const int i0 = page * kPage - L;
-    return tree ? slots_of_tree(i0, masks + (m - node0) * MW) : slots_of_chain(i0, m);
-  };
+  uint32_t* masks = (uint32_t*)lds;
+  if (tree) tree_masks(a, t, masks, (int*)lds + 16 * RPW * kTreeWords, 256);
 
   u32x4 kr[S], vr[S];
   f32x4 ksr[2], vsr[2];
   auto load = [&](int it) __attribute__((always_inline)) {
     const int id = __builtin_amdgcn_readlane(ids, it & 63);
     const bool bad = id < 0 || id >= a.c.pages;
-    const uint8_t* u = a.c.pool + ((long long)(bad ? 0 : id) * a.c.Hkv + kvh) * UNIT;
+    const uint8_t* u = a.c.pool + ((long long)(bad ? 0 : id) * a.c.Hkv + t.kvh) * UNIT;
 #pragma unroll
     for (int s = 0; s < S; ++s) kr[s] = *(const u32x4*)(u + s * 1024 + lane * 16);
 #pragma unroll
     for (int s = 0; s < S; ++s) vr[s] = *(const u32x4*)(u + kPage * HD + s * 1024 + lane * 16);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      ksr[t] = *(const f32x4*)(u + 2 * kPage * HD + 64 * t + 16 * lg);
-      vsr[t] = *(const f32x4*)(u + 2 * kPage * HD + 4 * kPage + 64 * t + 16 * lg);
+    for (int h = 0; h < 2; ++h) {
+      ksr[h] = *(const f32x4*)(u + 2 * kPage * HD + 64 * h + 16 * lg);
+      vsr[h] = *(const f32x4*)(u + 2 * kPage * HD + 4 * kPage + 64 * h + 16 * lg);
     }
     if (bad) {   // its keys have no value: rows that see one are NaN
       const float nan = __uint_as_float(0x7fc00000u);
@@ -215,177 +436,216 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
     }
   };
 
-  f32x4 acc[RPW][DT];
-  float m_run[RPW], l_run[RPW];
+  auto step = [&](auto masked, int it) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const int page = t.beg + kw + KW * it;
+    f32x4 sc[RPW][2];
 #pragma unroll
-  for (int r = 0; r < RPW; ++r) {
-#pragma unroll
-    for (int t = 0; t < DT; ++t) acc[r][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    // running maximum (log2 units) and sum.  The exponentials use a maximum
-    // that may lie up to kLazy below the true one, so O is rescaled rarely.
-    m_run[r] = -INFINITY;
-    l_run[r] = over ? __uint_as_float(0x7fc00000u) : 0.f;
-  }
-
-  if (npages > 0) load(0);
-  for (int it = 0; it < npages; ++it) {
-    const int page = beg + kw + KW * it;
-    // scores of this page
-    f32x4 sA[RPW], sB[RPW];
-#pragma unroll
-    for (int r = 0; r < RPW; ++r) sA[r] = sB[r] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < RPW; ++r) sc[r][0] = sc[r][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      const bf16x8 kA = codes8<FMT>(kr[s].x, kr[s].y), kB = codes8<FMT>(kr[s].z, kr[s].w);
-#pragma unroll
-      for (int r = 0; r < RPW; ++r)
-#pragma unroll
-        for (int pl = 0; pl < QP; ++pl) {
-          sA[r] = mfma16(kA, qf[r][s][pl], sA[r]);
-          sB[r] = mfma16(kB, qf[r][s][pl], sB[r]);
-        }
+      score_step(row, s, codes_f16<FMT>(kr[s].x, kr[s].y), codes_f16<FMT>(kr[s].z, kr[s].w), sc);
     }
-    float ks[8], vs[8];
+    const f32x4 ks[2] = {ksr[0], ksr[1]}, vs[2] = {vsr[0], vsr[1]};
+    if constexpr (FMT == kE4M3 && MASKED) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      ks[e] = ksr[e >> 2][e & 3] * a.scale_log2;
-      vs[e] = vsr[e >> 2][e & 3];
+      for (int s = 0; s < S; ++s) vr[s] = hold_values(vr[s], t.L + t.nb - page * kPage, lg);
     }
     bf16x8 vf[DT];
-    const bool masked = (page + 1) * kPage > L;   // uniform: the page holds nodes
-    if (FMT == kE4M3 && masked) {
-      // slots past the last node were never written: a code there may be a NaN
-      const int held = L + nb - page * kPage;
-      const unsigned hm = held >= 32 ? ~0u : (1u << held) - 1u;
-      const unsigned mA = byte_mask(hm >> (4 * lg)), mB = byte_mask(hm >> (16 + 4 * lg));
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        vr[s].x &= mA;
-        vr[s].y &= mB;
-        vr[s].z &= mA;
-        vr[s].w &= mB;
-      }
-    }
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      vf[2 * s] = codes8<FMT>(vr[s].x, vr[s].y);
-      vf[2 * s + 1] = codes8<FMT>(vr[s].z, vr[s].w);
+      vf[2 * s] = codes_bf16<FMT>(vr[s].x, vr[s].y);
+      vf[2 * s + 1] = codes_bf16<FMT>(vr[s].z, vr[s].w);
     }
     // the next page's loads are in flight during the rest
     if (it + 1 < npages) {
       if (((it + 1) & 63) == 0) fetch_ids(it + 1);
       load(it + 1);
     }
+    bf16x8 pf[RPW][Row::PP];
+    page_softmax<MASKED>(row, sc, ks, vs, tree, page * kPage - t.L, t.node0, masks, lg, pf);
 #pragma unroll
-    for (int r = 0; r < RPW; ++r) {
-      unsigned vis = ~0u;
-      if (masked) vis = visible(page, node[r]) >> (4 * lg);
-      float sv[8], mt = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sv[e] = (e < 4 ? sA[r][e & 3] : sB[r][e & 3]) * ks[e];
-        if (masked && !(vis >> (e < 4 ? e : 12 + e) & 1u)) sv[e] = -INFINITY;
-        mt = fmaxf(mt, sv[e]);
-      }
-      mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
-      mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-      const bool raise = mt > m_run[r] + kLazy;   // true for the first visible key
-      if (__ballot(raise)) {
-        const float m_to = raise ? mt : m_run[r];
-        const float corr = m_to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[r] - m_to);
-        l_run[r] *= corr;
-#pragma unroll
-        for (int t = 0; t < DT; ++t) acc[r][t] *= corr;
-        m_run[r] = m_to;
-      }
-      const float m_use = m_run[r] == -INFINITY ? 0.f : m_run[r];
-      bf16x8 pf[PP];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(sv[e] - m_use);
-        l_run[r] += p;
-        float x = p * vs[e];
-        if (masked && !(vis >> (e < 4 ? e : 12 + e) & 1u)) x = 0.f;   // its scale may be anything
-#pragma unroll
-        for (int pl = 0; pl < PP; ++pl) {
-          const bf16 hi = (bf16)x;
-          pf[pl][e] = hi;
-          x -= (float)hi;
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < DT; ++t)
-#pragma unroll
-        for (int pl = 0; pl < PP; ++pl) acc[r][t] = mfma16(vf[t], pf[pl], acc[r][t]);
-    }
-  }
+    for (int d = 0; d < DT; d += 2) value_step(row, d, vf[d], vf[d + 1], pf);
+  };
+  // the pages of prompt tokens only, then those that hold nodes
+  const int plain = min(npages, max(0, (t.L / kPage - t.beg - kw + KW - 1) / KW));
+  if (npages > 0) load(0);
+  int it = 0;
+  for (; it < plain; ++it) step(std::false_type{}, it);
+  for (; it < npages; ++it) step(std::true_type{}, it);
 
 #pragma unroll
-  for (int r = 0; r < RPW; ++r) {
-    l_run[r] += __shfl_xor(l_run[r], 16, 64);
-    l_run[r] += __shfl_xor(l_run[r], 32, 64);
-  }
-  if constexpr (KW > 1) {
-    // key groups 1.. hand (m, l, O) to group 0, which adds them in order
-    __syncthreads();   // the masks are no longer read
-    if (has_rows && kw > 0) {
+  for (int r = 0; r < RPW; ++r) row[r].finish();
+  // waves 1.. hand (m, l, O) to wave 0, which adds them in order
+  __syncthreads();   // the masks are no longer read
+  if (kw > 0) {
 #pragma unroll
-      for (int r = 0; r < RPW; ++r) {
-        float* x = lds + ((rt * (KW - 1) + kw - 1) * RPW + r) * SLOT;
-        x[lane] = m_run[r];
-        x[64 + lane] = l_run[r];
+    for (int r = 0; r < RPW; ++r) {
+      float* x = lds + ((kw - 1) * RPW + r) * SLOT;
+      x[lane] = row[r].m;
+      x[64 + lane] = row[r].l;
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[(2 + 4 * t + e) * 64 + lane] = acc[r][t][e];
-      }
+        for (int e = 0; e < 4; ++e) x[(2 + 4 * d + e) * 64 + lane] = row[r].acc[d][e];
     }
+  }
+  __syncthreads();
+  if (kw > 0) return;
+#pragma unroll
+  for (int r = 0; r < RPW; ++r) {
+#pragma unroll
+    for (int k = 1; k < KW; ++k) {
+      const float* x = lds + ((k - 1) * RPW + r) * SLOT;
+      const float mq = x[lane], lq = x[64 + lane];
+      const float mn = fmaxf(row[r].m, mq);
+      const float s0 = row[r].m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(row[r].m - mn);
+      const float s1 = mq == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mq - mn);
+      row[r].l = row[r].l * s0 + lq * s1;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          row[r].acc[d][e] = row[r].acc[d][e] * s0 + x[(2 + 4 * d + e) * 64 + lane] * s1;
+      row[r].m = mn;
+    }
+    row[r].store(a, t, lg);
+  }
+}
+
+// Workgroup = (key split, prompt x KV head, group of a.wg_tiles row tiles);
+// wave w takes tiles w RPW .. .  A page is converted once for all waves: its
+// codes come in as 16 bytes a thread, two pages before they are needed, and go
+// to LDS as f16 (keys) and bf16 (values) in operand order.
+template <int HD, int FMT, typename QT, int RPW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RPW == 1 ? 3 : 2))) void tree_many_kernel(
+    TreeAttnArgs a) {
+  using Row = RowTile<HD, QT>;
+  constexpr int NT = 256, W = 4;
+  constexpr int S = Row::S, DT = Row::DT;
+  constexpr int UNIT = kvq_unit_bytes(HD);
+  constexpr int CH = 2 * S * 64;                     // 16-byte chunks of codes in a unit
+  constexpr int PER = (CH + NT - 1) / NT;
+  constexpr int ROWS = 16 * W * RPW;
+  __shared__ __attribute__((aligned(16))) u32x4 tile[2][2 * CH];   // [keys: S][half] [values: DT], 64 lanes each
+  __shared__ __attribute__((aligned(16))) float scale[2][2 * kPage];
+  __shared__ uint32_t masks[ROWS * kTreeWords];
+  __shared__ int par[kTreeMax];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  const TreeSpan t = tree_span(a, a.wg_tiles);
+  if (t.none) return;   // uniform over the workgroup
+  const int npages = t.end - t.beg;
+  const int wrow = t.row0 + 16 * RPW * wave;
+  const int wend = min(t.row0 + 16 * a.wg_tiles, t.nrows);
+  const bool has_rows = wrow < wend;
+
+  const int* table = a.c.table + (long long)t.b * a.c.table_stride + t.beg;
+  // Two pages in flight.  Loads past the last page repeat it: without a branch
+  // the compiler knows how many are outstanding, and waits for the older page
+  // alone.
+  u32x4 raw[2][PER];
+  float sraw[2];
+  bool bad[2] = {false, false};
+  int id_next = npages > 0 ? table[0] : 0;   // of the page that is loaded next: a scalar load, one step ahead
+  auto load = [&](int it, int slot) __attribute__((always_inline)) {
+    const int id = id_next;
+    id_next = table[min(it + 1, npages - 1)];
+    bad[slot] = id < 0 || id >= a.c.pages;
+    const uint8_t* u = a.c.pool + ((long long)(bad[slot] ? 0 : id) * a.c.Hkv + t.kvh) * UNIT;
+#pragma unroll
+    for (int c = 0; c < PER; ++c)
+      if (CH % NT == 0 || tid + NT * c < CH) raw[slot][c] = *((const u32x4*)u + tid + NT * c);
+    sraw[slot] = *((const float*)(u + 2 * kPage * HD) + lane);
+  };
+  auto put = [&](int it, int buf) __attribute__((always_inline)) {
+    const int page = t.beg + it;
+#pragma unroll
+    for (int c = 0; c < PER; ++c) {
+      const int i = tid + NT * c;
+      if (CH % NT != 0 && i >= CH) continue;
+      const int s = i >> 6;
+      union {
+        f16x8 h;
+        bf16x8 b;
+        u32x4 u;
+      } x, y;
+      const u32x4 w = raw[buf][c];
+      if (CH % (2 * NT) == 0 ? c < PER / 2 : s < S) {   // uniform over a wave
+        x.h = codes_f16<FMT>(w.x, w.y);
+        y.h = codes_f16<FMT>(w.z, w.w);
+      } else {
+        u32x4 v = w;
+        if (FMT == kE4M3 && (page + 1) * kPage > t.L) v = hold_values(v, t.L + t.nb - page * kPage, lg);
+        x.b = codes_bf16<FMT>(v.x, v.y);
+        y.b = codes_bf16<FMT>(v.z, v.w);
+      }
+      tile[buf][(2 * s) * 64 + lane] = x.u;
+      tile[buf][(2 * s + 1) * 64 + lane] = y.u;
+    }
+    // a page that does not exist: rows that see one of its keys are NaN
+    if (wave == 0) scale[buf][lane] = bad[buf] && lane < kPage ? __uint_as_float(0x7fc00000u) : sraw[buf];
+  };
+
+  if (npages > 0) {
+    load(0, 0);
+    load(1, 1);
+  }
+  Row row[RPW];
+#pragma unroll
+  for (int r = 0; r < RPW; ++r) {
+    row[r].init(a, t, wrow + 16 * r + lr, lg);
+    row[r].valid = wrow + 16 * r + lr < wend;
+  }
+  // the last node of the wave's rows: later pages hold nothing for it
+  const int wlast = (min(wrow + 16 * RPW, wend) - 1) / a.G;
+  const bool tree = a.parents != nullptr && a.n > 1;
+  if (tree) tree_masks(a, t, masks, par, NT);
+  if (npages > 0) put(0, 0);
+  __syncthreads();
+
+  auto step = [&](auto masked, int it, int buf) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const int page = t.beg + it;
+    load(it + 2, buf);
+    if (has_rows && !(MASKED && page * kPage > t.L + wlast)) {
+      f32x4 sc[RPW][2];
+#pragma unroll
+      for (int r = 0; r < RPW; ++r) sc[r][0] = sc[r][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+        score_step(row, s, *(const f16x8*)&tile[buf][(2 * s) * 64 + lane],
+                   *(const f16x8*)&tile[buf][(2 * s + 1) * 64 + lane], sc);
+      const f32x4 ks[2] = {*(const f32x4*)&scale[buf][4 * lg], *(const f32x4*)&scale[buf][16 + 4 * lg]};
+      const f32x4 vs[2] = {*(const f32x4*)&scale[buf][kPage + 4 * lg], *(const f32x4*)&scale[buf][kPage + 16 + 4 * lg]};
+      bf16x8 pf[RPW][Row::PP];
+      page_softmax<MASKED>(row, sc, ks, vs, tree, page * kPage - t.L, t.node0, masks, lg, pf);
+#pragma unroll
+      for (int d = 0; d < DT; d += 2)
+        value_step(row, d, *(const bf16x8*)&tile[buf][CH + d * 64 + lane],
+                   *(const bf16x8*)&tile[buf][CH + (d + 1) * 64 + lane], pf);
+    }
+    put(it + 1, buf ^ 1);
     __syncthreads();
-    if (kw > 0) return;
+  };
+  // Pairs of pages of prompt tokens only, then the pages that hold nodes (and
+  // one before them, if the plain ones are odd).
+  const int plain = min(npages, max(0, t.L / kPage - t.beg)) & ~1;
+  int it = 0;
+  for (; it < plain; it += 2) {
+    step(std::false_type{}, it, 0);
+    step(std::false_type{}, it + 1, 1);
+  }
+  for (; it < npages; it += 2) {
+    step(std::true_type{}, it, 0);
+    if (it + 1 < npages) step(std::true_type{}, it + 1, 1);
   }
   if (!has_rows) return;
-  if constexpr (KW > 1) {
-#pragma unroll
-    for (int k = 1; k < KW; ++k)
-#pragma unroll
-      for (int r = 0; r < RPW; ++r) {
-        const float* x = lds + ((rt * (KW - 1) + k - 1) * RPW + r) * SLOT;
-        const float mq = x[lane], lq = x[64 + lane];
-        const float mn = fmaxf(m_run[r], mq);
-        const float s0 = m_run[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[r] - mn);
-        const float s1 = mq == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mq - mn);
-        l_run[r] = l_run[r] * s0 + lq * s1;
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[r][t][e] = acc[r][t][e] * s0 + x[(2 + 4 * t + e) * 64 + lane] * s1;
-        m_run[r] = mn;
-      }
-  }
 #pragma unroll
   for (int r = 0; r < RPW; ++r) {
-    if (!valid[r]) continue;
-    const long long row = ((long long)b * a.n + node[r]) * a.H + qrow[r];
-    // lane (row lr, lg) holds dims 16 t + 4 lg .. +3
-    if (a.nsplit == 1) {
-      const float inv = 1.f / l_run[r];
-      QT* o = (QT*)a.out + row * HD + 4 * lg;
-#pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const f32x4 y = acc[r][t] * inv;
-        if constexpr (sizeof(QT) == 4) *(f32x4*)(o + 16 * t) = y;
-        else *(bf16x4*)(o + 16 * t) = (bf16x4){(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
-      }
-    } else {
-      const long long prow = (long long)split * a.c.B * a.n * a.H + row;
-      float* po = a.part_o + prow * HD + 4 * lg;
-#pragma unroll
-      for (int t = 0; t < DT; ++t) *(f32x4*)(po + 16 * t) = acc[r][t];
-      if (lg == 0) {
-        a.part_ml[prow * 2] = m_run[r];
-        a.part_ml[prow * 2 + 1] = l_run[r];
-      }
-    }
+    row[r].finish();
+    row[r].store(a, t, lg);
   }
 }
 
@@ -440,11 +700,10 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeAttnArgs a) {
 template <int HD, int FMT, typename QT>
 hipError_t tree_attn_rows(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t st) {
   const unsigned grid = (unsigned)((long long)p.row_groups * p.nsplit * a.c.B * a.c.Hkv);
-  if (p.rpw == 1 && p.kw == 4) tree_attn_kernel<HD, FMT, QT, 1, 4><<<grid, 256, 0, st>>>(a);
-  else if (p.rpw == 2 && p.kw == 4) tree_attn_kernel<HD, FMT, QT, 2, 4><<<grid, 256, 0, st>>>(a);
-  else if (p.rpw == 2 && p.kw == 2) tree_attn_kernel<HD, FMT, QT, 2, 2><<<grid, 256, 0, st>>>(a);
-  else if (p.rpw == 2 && p.kw == 1) tree_attn_kernel<HD, FMT, QT, 2, 1><<<grid, 256, 0, st>>>(a);
-  else return hipErrorInvalidValue;
+  if (p.few == 1) tree_few_kernel<HD, FMT, QT, 1><<<grid, 256, 0, st>>>(a);
+  else if (p.few == 2) tree_few_kernel<HD, FMT, QT, 2><<<grid, 256, 0, st>>>(a);
+  else if (p.rpw == 1) tree_many_kernel<HD, FMT, QT, 1><<<grid, 256, 0, st>>>(a);
+  else tree_many_kernel<HD, FMT, QT, 2><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const long long rows = (long long)a.c.B * a.n * a.H;

@@ -90,7 +90,7 @@ static void visibility() {
     uint32_t mask[kTreeWords] = {};
     for (int m = 0; m <= node; ++m)
       if (m == node || g() % 3 == 0) mask[m >> 5] |= 1u << (m & 31);
-    for (int page = L / kPage; page <= (L + n - 1) / kPage; ++page) {
+    for (int page = 0; page <= (L + n - 1) / kPage; ++page) {
       const int i0 = page * kPage - L;
       const uint32_t chain = slots_of_chain(i0, node), tree = slots_of_tree(i0, mask);
       for (int s = 0; s < kPage; ++s) {
