@@ -20,6 +20,8 @@
 // One workgroup per prompt: the walk is a chain of decisions, and only the
 // rows it rejects at, and the last one, are read.  The probabilities of all
 // children are fetched at once first, so that the walk itself stays in LDS.
+// Latency bounds it, so a row's loads are all in flight together, and rows of
+// up to 32768 ids stay in registers for the node's further sums and the draw.
 #include "tree.h"
 
 namespace cdsl {
@@ -27,8 +29,10 @@ namespace cdsl {
 namespace {
 
 constexpr int NT = 1024, NW = NT / 64;
-constexpr int BLK = 4 * NT;                     // ids per block: four a thread
-constexpr int kSegs = kAcceptMaxVocab / BLK * NW;   // (block, wave) sums at most
+constexpr int RUN = 1024;                       // consecutive ids of a wave in a chunk: 16 a lane
+constexpr int CHUNK = NW * RUN;
+constexpr int kSegs = kAcceptMaxVocab / RUN;    // (chunk, wave) sums at most
+constexpr int kHeld = 2;                        // chunks that registers hold
 
 __device__ __forceinline__ double wave_sum_d(double v) {
 #pragma unroll
@@ -36,18 +40,44 @@ __device__ __forceinline__ double wave_sum_d(double v) {
   return v;
 }
 
-// four entries of a row from id i on (0 past the end)
-__device__ __forceinline__ void row4(const float* row, int i, int V, float (&x)[4]) {
-  if (i + 4 <= V) {
-    const f32x4u t = *(const f32x4u*)(row + i);
+// Sixteen entries of a row: four at i, i + 256, i + 512, i + 768 (0 past the end).
+struct Piece {
+  float x[4][4];
+  __device__ __forceinline__ void load(const float* row, int i, int V) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = t[e];
-  } else {
+    for (int u = 0; u < 4; ++u) {
+      const int at = i + 256 * u;
+      if (at + 4 <= V) {
+        const f32x4u t = *(const f32x4u*)(row + at);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = i + e < V ? row[i + e] : 0.f;
+        for (int e = 0; e < 4; ++e) x[u][e] = t[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[u][e] = at + e < V ? row[at + e] : 0.f;
+      }
+    }
   }
+};
+
+// max(0, p - c q); a NaN stays one
+__device__ __forceinline__ double weight(float p, float q, double c) {
+  const double d = fma(-c, (double)q, (double)p);
+  return d < 0. ? 0. : d;
+}
+__device__ __forceinline__ double weights(const Piece& p, const Piece& q, double c) {
+  double a = 0., b = 0.;
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      a += weight(p.x[u][e], q.x[u][e], c);
+      b += weight(p.x[u][e + 1], q.x[u][e + 1], c);
+    }
+  return a + b;
 }
 
+// HELD: V <= kHeld * CHUNK.
+template <bool HELD>
 __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict__ p_all,
                                                          const float* __restrict__ q_all, int n, int V,
                                                          const int* __restrict__ tokens,
@@ -57,8 +87,7 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict
                                                          int* n_path, int* next_token) {
   __shared__ int par[kTreeMax], tok[kTreeMax], walk[kTreeMax];
   __shared__ float px[kTreeMax], qx[kTreeMax], us[kTreeMax];
-  __shared__ double part[kSegs];
-  __shared__ double wtot[NW];
+  __shared__ double part[HELD ? kHeld * NW : kSegs];
   __shared__ int hit, best_i[NW];
   __shared__ float best_v[NW];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
@@ -67,97 +96,117 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict
   for (int j = tid; j < nb; j += NT) {
     int c = j > 0 ? parents[row0 + j] : -1;
     const int x = tokens[row0 + j];
+    const float uj = u[row0 + j];
     if (c < 0 || c >= j || x < 0 || x >= V) c = -1;   // not a child that can be taken
     par[j] = c;
     tok[j] = x;
     if (c >= 0) {
       px[j] = p_all[(row0 + c) * V + x];
       qx[j] = q_all[(row0 + c) * V + x];
-      us[j] = u[row0 + j];
+      us[j] = uj;
     }
   }
   if (tid == 0) walk[0] = 0, hit = -1;
   __syncthreads();
 
-  const int nblk = (V + BLK - 1) / BLK;
+  const int chunks = (V + CHUNK - 1) / CHUNK, segs = chunks * NW;
+  const int at0 = wv * RUN + 4 * lane;   // this lane's first id of a chunk
   int cur = 0, len = 1, from = 1;
   double c = 0., N = 1., rest = 1.;
   const float* p = p_all + row0 * V;
   const float* q = q_all + row0 * V;
+  Piece hp[HELD ? kHeld : 1], hq[HELD ? kHeld : 1];
+  bool have_p = false, have_q = false;   // the held pieces are those of cur
 
-  // w = max(0, p - c q) of four ids
-  auto weights = [&](int i, double (&w)[4]) __attribute__((always_inline)) {
-    float x[4], y[4];
-    row4(p, i, V, x);
-    if (c > 0.) {
-      row4(q, i, V, y);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = fmax(0., fma(-c, (double)y[e], (double)x[e]));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = (double)x[e];
-    }
-  };
-  // part[block * NW + wave] and the sum over all ids
+  // part[chunk * NW + wave] and their sum, for the present c
   auto sum = [&]() __attribute__((always_inline)) -> double {
-    double mine = 0.;
-    for (int k = 0; k < nblk; ++k) {
-      double w[4];
-      weights(BLK * k + 4 * tid, w);
-      const double s = wave_sum_d((w[0] + w[1]) + (w[2] + w[3]));
-      if (lane == 0) part[k * NW + wv] = s;
-      mine += s;
+    __syncthreads();   // earlier readers of part are done
+    if constexpr (HELD) {
+      const bool lp = !have_p, lq = !have_q && c > 0.;
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        if (lp) hp[k].load(p, CHUNK * k + at0, V);
+        if (lq) hq[k].load(q, CHUNK * k + at0, V);
+        else if (c == 0.) hq[k] = Piece{};
+      }
+      have_p = true;
+      have_q = c > 0.;
+      double s[kHeld];
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) s[k] = wave_sum_d(weights(hp[k], hq[k], c));
+      if (lane == 0)
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+          if (k < chunks) part[k * NW + wv] = s[k];
+    } else {
+      // the next chunk's loads are in flight while one is added up
+      Piece np, nq{}, xp, xq{};
+      np.load(p, at0, V);
+      if (c > 0.) nq.load(q, at0, V);
+      for (int k = 0; k < chunks; ++k) {
+        xp = np;
+        xq = nq;
+        if (k + 1 < chunks) {
+          np.load(p, CHUNK * (k + 1) + at0, V);
+          if (c > 0.) nq.load(q, CHUNK * (k + 1) + at0, V);
+        }
+        const double s = wave_sum_d(weights(xp, xq, c));
+        if (lane == 0) part[k * NW + wv] = s;
+      }
     }
-    __syncthreads();   // earlier readers of wtot are done
-    if (lane == 0) wtot[wv] = mine;
     __syncthreads();
     double t = 0.;
-#pragma unroll
-    for (int k = 0; k < NW; ++k) t += wtot[k];
-    return t;
+    for (int k = lane; k < segs; k += 64) t += part[k];
+    return wave_sum_d(t);
   };
 
-  // Every wave walks alike, 64 nodes at a time.
-  bool none = false, summed = false;   // no mass left; part holds the sums of the present c
-  while (from < nb && !none) {
-    const int j0 = from & ~63, j = j0 + lane;
-    const unsigned long long kids = __ballot(j >= from && j < nb && par[j] == cur);
-    if (!kids) {
-      from = j0 + 64;
-      continue;
+  // Every wave walks alike, 64 nodes at a time, from one sum to the next.
+  bool none = false, done = false, summed = false;   // no mass left; walked; part holds the sums of the present c
+  while (true) {
+    int fell = -1;   // the child that is rejected next
+    while (from < nb && !none && fell < 0) {
+      const int j0 = from & ~63, j = j0 + lane;
+      const unsigned long long kids = __ballot(j >= from && j < nb && par[j] == cur);
+      if (!kids) {
+        from = j0 + 64;
+        continue;
+      }
+      const int k = j0 + __builtin_ctzll(kids);
+      from = k + 1;
+      if (!(rest > 0.)) continue;
+      const double pk = c > 0. ? weight(px[k], qx[k], c) / N : (double)px[k];
+      const double qk = (double)qx[k] / rest;
+      if (pk > 0. && (double)us[k] * qk <= pk) {
+        if (tid == 0) walk[len] = k;
+        ++len;
+        cur = k;
+        p = p_all + (row0 + k) * V;
+        q = q_all + (row0 + k) * V;
+        c = 0., N = 1., rest = 1.;
+        summed = have_p = have_q = false;
+      } else {
+        fell = k;
+      }
     }
-    const int k = j0 + __builtin_ctzll(kids);
-    from = k + 1;
-    if (!(rest > 0.)) continue;
-    const double pk = c > 0. ? fmax(0., fma(-c, (double)qx[k], (double)px[k])) / N : (double)px[k];
-    const double qk = (double)qx[k] / rest;
-    if (pk > 0. && (double)us[k] * qk <= pk) {
-      if (tid == 0) walk[len] = k;
-      ++len;
-      cur = k;
-      p = p_all + (row0 + k) * V;
-      q = q_all + (row0 + k) * V;
-      c = 0., N = 1., rest = 1.;
-      summed = false;
-      continue;
-    }
-    c += N / rest;
+    done = fell < 0;
+    if (!done) c += N / rest;
+    if (done && summed) break;
     N = sum();
+    if (done) break;
     summed = true;
     if (!replace) {
       // a token that an earlier sibling carried is out of q already
       bool twice = false;
-      for (int s = 0; s < k; s += 64) {
+      for (int s = 0; s < fell; s += 64) {
         const int e = s + lane;
-        twice = twice || __ballot(e < k && par[e] == cur && tok[e] == tok[k]);
+        twice = twice || __ballot(e < fell && par[e] == cur && tok[e] == tok[fell]);
       }
-      if (!twice) rest -= (double)qx[k];
+      if (!twice) rest -= (double)qx[fell];
     }
     if (!(N > 0.)) none = true;
   }
 
   // The draw: the first id whose running sum passes v * (sum).
-  if (!summed) N = sum();
   if (none) {
     // argmax p, lowest id on ties
     float bv = -INFINITY;
@@ -179,28 +228,32 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict
       hit = N == 0. ? bi : -1;
     }
   } else if (N > 0. && N < INFINITY) {
-    const int segs = nblk * NW;
-    const double T = (double)v[b] * N;
-    // the segment the draw falls in, and the sum before it: each lane of a
-    // wave takes a run of segments
-    const int run = (segs + 63) / 64;
-    double mine = 0.;
-    for (int s = lane * run; s < min(segs, lane * run + run); ++s) mine += part[s];
-    double incl = mine;
+    // first entry of a row of lanes whose running sum from `at` passes T (the
+    // last one with mass when rounding leaves T past the total), and the sum
+    // before it
+    auto locate = [&](double mine, double T, double& at) __attribute__((always_inline)) -> int {
+      double incl = mine;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double t = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += t;
-    }
-    double before = __shfl_up(incl, 1, 64);
-    if (lane == 0) before = 0.;
-    const unsigned long long past = __ballot(mine > 0. && incl > T), mass = __ballot(mine > 0.);
-    // rounding may leave T at the sum: then the last run with mass
-    const int src = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(mass | 1ull);
-    double at = __shfl(before, src, 64);
+      for (int o = 1; o < 64; o <<= 1) {
+        const double t = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += t;
+      }
+      double before = __shfl_up(incl, 1, 64);
+      if (lane == 0) before = 0.;
+      const unsigned long long past = __ballot(mine > 0. && at + incl > T), mass = __ballot(mine > 0.);
+      const int src = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(mass | 1ull);
+      at += __shfl(before, src, 64);
+      return mass ? src : -1;
+    };
+    const double T = (double)v[b] * N;
+    // each lane takes a run of segments
+    const int run = (segs + 63) / 64;
+    double mine = 0., at = 0.;
+    for (int s = lane * run; s < min(segs, lane * run + run); ++s) mine += part[s];
+    const int src = locate(mine, T, at);
     int seg = -1;
     double seg_at = at;
-    for (int s = src * run; s < min(segs, src * run + run); ++s) {
+    for (int s = src * run; src >= 0 && s < min(segs, src * run + run); ++s) {
       if (part[s] > 0.) {
         seg = s;
         seg_at = at;
@@ -208,32 +261,44 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict
       }
       at += part[s];
     }
-    if (seg >= 0 && wv == seg % NW) {
-      const int i0 = BLK * (seg / NW) + 4 * tid;
-      double w[4];
-      weights(i0, w);
-      const double own = (w[0] + w[1]) + (w[2] + w[3]);
-      double sc = own;
+    if (seg >= 0 && wv == seg % NW) {   // its wave: 4 x 64 lanes x 4 ids in order
+      const int i0 = CHUNK * (seg / NW) + at0;
+      Piece xp, xq{};
+      xp.load(p, i0, V);
+      if (c > 0.) xq.load(q, i0, V);
+      double t[4], w[4];
+      int pick = -1;
+      double pick_at = seg_at;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double t = __shfl_up(sc, o, 64);
-        if (lane >= o) sc += t;
-      }
-      double r = __shfl_up(sc, 1, 64);
-      if (lane == 0) r = 0.;
-      r += seg_at;
-      int at_e = -1, last_e = -1;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (w[e] > 0.) {
-          last_e = e;
-          if (at_e < 0 && r + w[e] > T) at_e = e;
+      for (int k = 0; k < 4; ++k) {
+        t[k] = (weight(xp.x[k][0], xq.x[k][0], c) + weight(xp.x[k][1], xq.x[k][1], c)) +
+               (weight(xp.x[k][2], xq.x[k][2], c) + weight(xp.x[k][3], xq.x[k][3], c));
+        const double all = wave_sum_d(t[k]);
+        if (all > 0. && !(pick >= 0 && seg_at > T)) {
+          pick = k;
+          pick_at = seg_at;
         }
-        r += w[e];
+        seg_at += all;
       }
-      const unsigned long long hits = __ballot(at_e >= 0), with = __ballot(last_e >= 0);
-      const int who = hits ? __builtin_ctzll(hits) : 63 - __builtin_clzll(with | 1ull);
-      if (lane == who && with) hit = i0 + (hits ? at_e : last_e);
+      double own = 0.;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k == pick) {
+          own = t[k];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = weight(xp.x[k][e], xq.x[k][e], c);
+        }
+      double lane_at = pick_at;
+      const int who = locate(own, T, lane_at);
+      if (lane == who) {
+        int e_at = -1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (w[e] > 0. && (e_at < 0 || !(lane_at > T))) e_at = e;
+          lane_at += w[e];
+        }
+        hit = i0 + 256 * pick + e_at;
+      }
     }
   }
   __syncthreads();
@@ -250,7 +315,12 @@ hipError_t tree_accept_launch(const float* p, const float* q, int B, int n, int 
                               const int* parents, const int* n_nodes, const float* u, const float* v, int replace,
                               int* path, int* n_path, int* next_token, hipStream_t st) {
   if (B == 0) return hipSuccess;
-  tree_accept_kernel<<<B, NT, 0, st>>>(p, q, n, V, tokens, parents, n_nodes, u, v, replace, path, n_path, next_token);
+  if (V <= kHeld * CHUNK)
+    tree_accept_kernel<true><<<B, NT, 0, st>>>(p, q, n, V, tokens, parents, n_nodes, u, v, replace, path, n_path,
+                                               next_token);
+  else
+    tree_accept_kernel<false><<<B, NT, 0, st>>>(p, q, n, V, tokens, parents, n_nodes, u, v, replace, path, n_path,
+                                                next_token);
   return hipGetLastError();
 }
 
