@@ -34,10 +34,26 @@ constexpr int CHUNK = NW * RUN;
 constexpr int kSegs = kAcceptMaxVocab / RUN;    // (chunk, wave) sums at most
 constexpr int kHeld = 2;                        // chunks that registers hold
 
+// Sum over a wave, the same bits in every lane: rotations within rows of 16,
+// then swaps of rows and halves (a shuffle through LDS takes five times as long).
+template <int CTRL>
+__device__ __forceinline__ double add_rotated(double v) {
+  const unsigned lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, false);
+  const unsigned hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, false);
+  return v + __hiloint2double(hi, lo);
+}
 __device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  v = add_rotated<0x128>(v);   // row_ror:8, 4, 2, 1
+  v = add_rotated<0x124>(v);
+  v = add_rotated<0x122>(v);
+  v = add_rotated<0x121>(v);
+  u32x2 lo = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
+  u32x2 hi = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
+  v = __hiloint2double(hi.x, lo.x) + __hiloint2double(hi.y, lo.y);
+  lo = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
+  hi = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
+  return __hiloint2double(hi.x, lo.x) + __hiloint2double(hi.y, lo.y);
 }
 
 // Sixteen entries of a row: four at i, i + 256, i + 512, i + 768 (0 past the end).
@@ -64,16 +80,21 @@ __device__ __forceinline__ double weight(float p, float q, double c) {
   const double d = fma(-c, (double)q, (double)p);
   return d < 0. ? 0. : d;
 }
+// Their sum as half of sum d + sum |d|: a subtraction and two additions an
+// entry, and a NaN stays one (the fp64 instructions bound a pass: a maximum
+// that keeps NaNs takes three).  Without an entry above 0 the two cancel to
+// exactly 0, since every partial sum has its negative.
 __device__ __forceinline__ double weights(const Piece& p, const Piece& q, double c) {
-  double a = 0., b = 0.;
+  double d = 0., a = 0.;
 #pragma unroll
   for (int u = 0; u < 4; ++u)
 #pragma unroll
-    for (int e = 0; e < 4; e += 2) {
-      a += weight(p.x[u][e], q.x[u][e], c);
-      b += weight(p.x[u][e + 1], q.x[u][e + 1], c);
+    for (int e = 0; e < 4; ++e) {
+      const double t = fma(-c, (double)q.x[u][e], (double)p.x[u][e]);
+      d += t;
+      a += fabs(t);
     }
-  return a + b;
+  return 0.5 * (d + a);
 }
 
 // HELD: V <= kHeld * CHUNK.
