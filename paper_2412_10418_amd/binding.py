@@ -277,38 +277,43 @@ _KVQ_FORMATS = {"int8": CDSL_KVQ_INT8, "e4m3": CDSL_KVQ_E4M3}
 _ROW_TYPES = {torch.float32: CDSL_F32, torch.bfloat16: CDSL_BF16}
 
 
-def _ints(t: Optional[torch.Tensor], shape, dev, name):
-    """Pointer of an int32 tensor of this shape on this device (None: null)."""
-    return _of(t, shape, torch.int32, dev, name) if t is not None else None
-
-
-def _of(t: torch.Tensor, shape, dtype, dev, name):
-    if t.dtype != dtype or t.device != dev or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}")
+def _of(t: torch.Tensor, shape, dtype, dev: int, name):
+    """Pointer of a contiguous tensor of this shape and type on device dev."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _strided(t: torch.Tensor, shape, dev, name):
+def _ints(t: Optional[torch.Tensor], shape, dev: int, name):
+    """_of for int32 (None: null)."""
+    return None if t is None else _of(t, shape, torch.int32, dev, name)
+
+
+def _strided(t: torch.Tensor, shape, dev: int, name):
     """Pointer and the (prompt, token) strides of rows [B, T, heads, hd] whose heads and dims are contiguous."""
-    if t.dtype not in _ROW_TYPES or t.device != dev or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be a float32 or bfloat16 tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}")
-    B, T, heads, hd = shape
+    if t.dtype not in _ROW_TYPES or t.get_device() != dev or t.shape != shape:
+        raise ValueError(f"{name} must be a float32 or bfloat16 tensor of shape {tuple(shape)} on device {dev}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
     sb, st, sh, sd = t.stride()
-    if sd != 1 or (heads > 1 and sh != hd):
+    if sd != 1 or (sh != shape[3] and shape[2] > 1):
         raise ValueError(f"{name}: heads and dims must be contiguous, got strides {t.stride()}")
-    return t.data_ptr(), sb if B > 1 else 0, st if T > 1 else 0
+    return t.data_ptr(), sb if shape[0] > 1 else 0, st if shape[1] > 1 else 0
 
 
-def _call(dev, name, *args):
+# the handle of a device's current stream, without the Stream object around it
+# (0.1 against 1.9 us, of the 10 that a short call takes)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _call(dev: int, fn, *args):
     """The library call on the current stream of the tensors' device."""
-    fn = getattr(lib(), name)
-    if dev.index == torch.cuda.current_device():
-        rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            rc = fn(*args, _raw_stream(dev))
     if rc != CDSL_OK:
         _check(rc)
 
@@ -317,6 +322,8 @@ class QuantCache:
     """The 8-bit paged cache of a batch of prompts: pool [layers, pages, heads, unit bytes] (uint8, see
     ``QuantCache.empty``), table [prompts, pages per prompt] (int32 page ids)."""
 
+    __slots__ = ("pool", "table", "head_dim", "fmt", "batch", "n_kv_heads", "device", "_c", "_ref")
+
     def __init__(self, pool: torch.Tensor, table: torch.Tensor, head_dim: int, fmt: str):
         if fmt not in _KVQ_FORMATS:
             raise ValueError(f"fmt must be one of {sorted(_KVQ_FORMATS)}, got {fmt!r}")
@@ -324,17 +331,18 @@ class QuantCache:
             raise ValueError("head_dim must be 32, 64 or 128")
         if pool.dim() != 4 or table.dim() != 2:
             raise ValueError("pool must be [layers, pages, heads, unit], table [prompts, pages]")
-        if not pool.is_cuda:
-            raise ValueError("pool must be a device tensor")
-        layers, pages, heads, unit = pool.shape
+        layers, pages, heads, unit = shape = pool.shape
+        batch, stride = table.shape
         if unit != 64 * head_dim + 256:
             raise ValueError(f"a unit has 64 * head_dim + 256 = {64 * head_dim + 256} bytes, the pool {unit}")
-        self.pool, self.table, self.head_dim, self.fmt = pool, table, head_dim, fmt
-        self.batch, self.n_kv_heads, self.device = table.shape[0], heads, pool.device
-        self._c = KVQ(_of(pool, pool.shape, torch.uint8, pool.device, "pool"), _ints(table, table.shape, pool.device,
-                                                                                  "table"),
-                      layers, pages, heads, head_dim, table.shape[0], table.shape[1], _KVQ_FORMATS[fmt])
+        dev = pool.get_device()
+        if dev < 0:
+            raise ValueError("pool must be a device tensor")
+        self._c = KVQ(_of(pool, shape, torch.uint8, dev, "pool"), _of(table, table.shape, torch.int32, dev, "table"),
+                      layers, pages, heads, head_dim, batch, stride, _KVQ_FORMATS[fmt])
         self._ref = C.addressof(self._c)
+        self.pool, self.table, self.head_dim, self.fmt = pool, table, head_dim, fmt
+        self.batch, self.n_kv_heads, self.device = batch, heads, dev
 
     @staticmethod
     def empty(layers: int, pages: int, n_kv_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
@@ -353,12 +361,12 @@ def cdsl_op_kvq_write(cache: QuantCache, K: torch.Tensor, V: torch.Tensor, start
     dev, B = cache.device, cache.batch
     if K.dim() != 4:
         raise ValueError("K must be [B, T, heads, hd]")
-    shape = (B, K.shape[1], cache.n_kv_heads, cache.head_dim)
-    if K.dtype != V.dtype:
+    if K.dtype is not V.dtype:
         raise ValueError(f"K and V must have one type, got {K.dtype} and {V.dtype}")
+    shape = (B, K.shape[1], cache.n_kv_heads, cache.head_dim)
     k, ksb, kst = _strided(K, shape, dev, "K")
     v, vsb, vst = _strided(V, shape, dev, "V")
-    _call(dev, "cdsl_op_kvq_write", cache._ref, layer, k, v, _ROW_TYPES[K.dtype], shape[1], ksb, kst, vsb, vst,
+    _call(dev, lib().cdsl_op_kvq_write, cache._ref, layer, k, v, _ROW_TYPES[K.dtype], shape[1], ksb, kst, vsb, vst,
           _ints(start, (B,), dev, "start"), _ints(count, (B,), dev, "count"))
 
 
@@ -372,12 +380,13 @@ def cdsl_op_kvq_read(cache: QuantCache, T: int, start: Optional[torch.Tensor] = 
         if dtype not in _ROW_TYPES:
             raise ValueError(f"dtype must be float32 or bfloat16, got {dtype}")
         make = torch.empty if count is None else torch.zeros
-        out = (make(shape, dtype=dtype, device=dev), make(shape, dtype=dtype, device=dev))
+        out = (make(shape, dtype=dtype, device=cache.pool.device), make(shape, dtype=dtype, device=cache.pool.device))
     K, V = out
     if K.dtype not in _ROW_TYPES:
         raise ValueError(f"out must be float32 or bfloat16, got {K.dtype}")
-    _call(dev, "cdsl_op_kvq_read", cache._ref, layer, _of(K, shape, K.dtype, dev, "K"), _of(V, shape, K.dtype, dev, "V"),
-          _ROW_TYPES[K.dtype], T, _ints(start, (B,), dev, "start"), _ints(count, (B,), dev, "count"))
+    _call(dev, lib().cdsl_op_kvq_read, cache._ref, layer, _of(K, shape, K.dtype, dev, "K"),
+          _of(V, shape, K.dtype, dev, "V"), _ROW_TYPES[K.dtype], T, _ints(start, (B,), dev, "start"),
+          _ints(count, (B,), dev, "count"))
     return K, V
 
 
@@ -391,14 +400,15 @@ def cdsl_op_tree_attention(cache: QuantCache, q: torch.Tensor, lens: torch.Tenso
     dev, B, hd = cache.device, cache.batch, cache.head_dim
     if q.dim() != 4:
         raise ValueError("q must be [B, n, H, hd]")
-    shape = (B, q.shape[1], q.shape[2], hd)
-    n, H = shape[1], shape[2]
+    n, H = q.shape[1], q.shape[2]
+    shape = (B, n, H, hd)
     ptr, qsb, qst = _strided(q, shape, dev, "q")
     if out is None:
-        out = (torch.empty if n_nodes is None else torch.zeros)(shape, dtype=q.dtype, device=dev)
-    need = lib().cdsl_op_tree_attention_workspace(B, n, H, cache.n_kv_heads, hd, max_len)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _call(dev, "cdsl_op_tree_attention", cache._ref, layer, ptr, _ROW_TYPES[q.dtype], n, H, qsb, qst,
+        out = (torch.empty_like if n_nodes is None else torch.zeros_like)(q, memory_format=torch.contiguous_format)
+    L = lib()
+    need = L.cdsl_op_tree_attention_workspace(B, n, H, cache.n_kv_heads, hd, max_len)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _call(dev, L.cdsl_op_tree_attention, cache._ref, layer, ptr, _ROW_TYPES[q.dtype], n, H, qsb, qst,
           _of(lens, (B,), torch.int32, dev, "lens"), _ints(n_nodes, (B,), dev, "n_nodes"),
           _ints(parents, (B, n), dev, "parents"), hd ** -0.5 if scale is None else scale, max_len,
           _of(out, shape, q.dtype, dev, "out"), ws.data_ptr() if need else None, need)
@@ -410,18 +420,18 @@ def cdsl_op_tree_accept(target_probs: torch.Tensor, draft_probs: torch.Tensor, t
                         n_nodes: Optional[torch.Tensor] = None, replace: bool = True):
     """target_probs, draft_probs [B, n, V], tokens, parents, u [B, n], v [B]; returns (path [B, n], n_path [B],
     next_token [B])."""
-    if target_probs.dim() != 3 or not target_probs.is_cuda:
+    dev = target_probs.get_device()
+    if target_probs.dim() != 3 or dev < 0:
         raise ValueError("target_probs must be a device tensor [B, n, V]")
-    dev = target_probs.device
-    B, n, V = target_probs.shape
-    out = torch.empty(B * (n + 2), dtype=torch.int32, device=dev)
+    B, n, V = shape = target_probs.shape
+    out = torch.empty(B * (n + 2), dtype=torch.int32, device=target_probs.device)
     path, n_path, token = out[:B * n].view(B, n), out[B * n:B * n + B], out[B * n + B:]
-    _call(dev, "cdsl_op_tree_accept", _of(target_probs, (B, n, V), torch.float32, dev, "target_probs"),
-          _of(draft_probs, (B, n, V), torch.float32, dev, "draft_probs"), B, n, V,
+    at = out.data_ptr()
+    _call(dev, lib().cdsl_op_tree_accept, _of(target_probs, shape, torch.float32, dev, "target_probs"),
+          _of(draft_probs, shape, torch.float32, dev, "draft_probs"), B, n, V,
           _of(tokens, (B, n), torch.int32, dev, "tokens"), _of(parents, (B, n), torch.int32, dev, "parents"),
           _ints(n_nodes, (B,), dev, "n_nodes"), _of(u, (B, n), torch.float32, dev, "u"),
-          _of(v, (B,), torch.float32, dev, "v"), 1 if replace else 0, path.data_ptr(), n_path.data_ptr(),
-          token.data_ptr())
+          _of(v, (B,), torch.float32, dev, "v"), 1 if replace else 0, at, at + 4 * B * n, at + 4 * B * (n + 1))
     return path, n_path, token
 
 
@@ -430,10 +440,10 @@ def cdsl_op_kvq_keep(cache: QuantCache, lens: torch.Tensor, path: torch.Tensor, 
     dev, B = cache.device, cache.batch
     if path.dim() != 2:
         raise ValueError("path must be [B, n]")
-    new = torch.empty(B, dtype=torch.int32, device=dev)
-    _call(dev, "cdsl_op_kvq_keep", cache._ref, _of(lens, (B,), torch.int32, dev, "lens"),
-          _ints(path, (B, path.shape[1]), dev, "path"), _of(n_path, (B,), torch.int32, dev, "n_path"), path.shape[1],
-          new.data_ptr())
+    new = torch.empty_like(lens)
+    _call(dev, lib().cdsl_op_kvq_keep, cache._ref, _of(lens, (B,), torch.int32, dev, "lens"),
+          _of(path, (B, path.shape[1]), torch.int32, dev, "path"), _of(n_path, (B,), torch.int32, dev, "n_path"),
+          path.shape[1], new.data_ptr())
     return new
 
 
