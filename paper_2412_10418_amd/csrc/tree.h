@@ -38,18 +38,18 @@ struct TreeAttnArgs {
   float* part_o;           // [nsplit][B * n * H][hd]
   float* part_ml;          // [nsplit][B * n * H][2]
   int nsplit, row_groups;
+  int split_pages;         // pages per key split, at least
   int wg_tiles;            // row tiles per workgroup (tree_many_kernel)
 };
 
 struct TreeAttnPlan {
   int few;                 // 1, 2: tree_few_kernel with so many row tiles; 0: tree_many_kernel
   int rpw, wg_tiles;       // its row tiles per wave and per workgroup
-  int row_groups, nsplit;
+  int row_groups, nsplit, split_pages;
   size_t workspace;
 };
 
-// The workspace does not depend on dtype.
-TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, int dtype);
+TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len);
 hipError_t tree_attn_launch(TreeAttnArgs a, const TreeAttnPlan& p, int dtype, void* workspace, hipStream_t st);
 
 constexpr int kAcceptMaxVocab = 1 << 20;

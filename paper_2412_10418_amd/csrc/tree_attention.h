@@ -135,6 +135,18 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs& a, int tiles) 
   const int pair = chunk / a.nsplit;
   t.b = pair / a.c.Hkv;
   t.kvh = pair % a.c.Hkv;
+  // Prompts of unlike lengths: the longest first, so that the last workgroups
+  // to start are short (one lane a prompt finds its place).
+  if (a.nsplit == 1 && a.c.B > 1 && a.c.B <= 64) {
+    const int lane = threadIdx.x & 63;
+    const int len = lane < a.c.B ? a.lens[lane] : 0;
+    int place = 0;
+    for (int j = 0; j < a.c.B; ++j) {
+      const int l = __builtin_amdgcn_readlane(len, j);
+      place += l > len || (l == len && j < lane) ? 1 : 0;
+    }
+    t.b = __builtin_ctzll(__ballot(lane < a.c.B && place == t.b));
+  }
   t.nb = a.n_nodes ? min(max(a.n_nodes[t.b], 0), a.n) : a.n;
   t.nrows = t.nb * a.G;
   t.row0 = rg * 16 * tiles;
@@ -145,9 +157,10 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs& a, int tiles) 
   // a prompt that its table cannot hold has no answer: NaN, and no page read
   t.over = (long long)t.L + t.nb > (long long)a.c.table_stride * kPage;
   const int pages = t.over ? 0 : (t.L + t.nb + kPage - 1) / kPage;
-  const int per = (pages + a.nsplit - 1) / a.nsplit;
-  t.beg = t.split * per;
-  t.end = t.over ? 0 : min(min(t.beg + per, pages), (t.L + t.node1) / kPage + 1);
+  // splits of one size whatever the prompt's length: those past its end are empty
+  const int per = max(a.split_pages, (pages + a.nsplit - 1) / a.nsplit);
+  t.beg = (int)min((long long)t.split * per, (long long)pages);
+  t.end = t.over ? 0 : (int)min(min((long long)t.beg + per, (long long)pages), (long long)((t.L + t.node1) / kPage + 1));
   return t;
 }
 
@@ -417,23 +430,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
 
   u32x4 kr[S], vr[S];
   f32x4 ksr[2], vsr[2];
-  auto load = [&](int it) __attribute__((always_inline)) {
+  const uint8_t* unit = nullptr;   // of the page that is loaded
+  bool bad = false, next_bad = false;
+  auto load_keys = [&](int it) __attribute__((always_inline)) {
     const int id = __builtin_amdgcn_readlane(ids, it & 63);
-    const bool bad = id < 0 || id >= a.c.pages;
-    const uint8_t* u = a.c.pool + ((long long)(bad ? 0 : id) * a.c.Hkv + t.kvh) * UNIT;
+    next_bad = id < 0 || id >= a.c.pages;
+    unit = a.c.pool + ((long long)(next_bad ? 0 : id) * a.c.Hkv + t.kvh) * UNIT;
 #pragma unroll
-    for (int s = 0; s < S; ++s) kr[s] = *(const u32x4*)(u + s * 1024 + lane * 16);
-#pragma unroll
-    for (int s = 0; s < S; ++s) vr[s] = *(const u32x4*)(u + kPage * HD + s * 1024 + lane * 16);
+    for (int s = 0; s < S; ++s) kr[s] = *(const u32x4*)(unit + s * 1024 + lane * 16);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      ksr[h] = *(const f32x4*)(u + 2 * kPage * HD + 64 * h + 16 * lg);
-      vsr[h] = *(const f32x4*)(u + 2 * kPage * HD + 4 * kPage + 64 * h + 16 * lg);
+      ksr[h] = *(const f32x4*)(unit + 2 * kPage * HD + 64 * h + 16 * lg);
+      vsr[h] = *(const f32x4*)(unit + 2 * kPage * HD + 4 * kPage + 64 * h + 16 * lg);
     }
-    if (bad) {   // its keys have no value: rows that see one are NaN
-      const float nan = __uint_as_float(0x7fc00000u);
-      ksr[0] = ksr[1] = (f32x4){nan, nan, nan, nan};
-    }
+  };
+  auto load_values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) vr[s] = *(const u32x4*)(unit + kPage * HD + s * 1024 + lane * 16);
   };
 
   auto step = [&](auto masked, int it) __attribute__((always_inline)) {
@@ -446,30 +459,54 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
     for (int s = 0; s < S; ++s) {
       score_step(row, s, codes_f16<FMT>(kr[s].x, kr[s].y), codes_f16<FMT>(kr[s].z, kr[s].w), sc);
     }
-    const f32x4 ks[2] = {ksr[0], ksr[1]}, vs[2] = {vsr[0], vsr[1]};
+    f32x4 ks[2] = {ksr[0], ksr[1]};
+    const f32x4 vs[2] = {vsr[0], vsr[1]};
+    if (bad) {   // its keys have no value: rows that see one are NaN
+      const float nan = __uint_as_float(0x7fc00000u);
+      ks[0] = ks[1] = (f32x4){nan, nan, nan, nan};
+    }
     if constexpr (FMT == kE4M3 && MASKED) {
 #pragma unroll
       for (int s = 0; s < S; ++s) vr[s] = hold_values(vr[s], t.L + t.nb - page * kPage, lg);
     }
-    bf16x8 vf[DT];
+    // The next page's loads are in flight during the rest: all of them where
+    // there is room for this page's values as bf16, else its keys'.
+    bf16x8 vf[RPW == 1 ? DT : 1];
+    if constexpr (RPW == 1) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      vf[2 * s] = codes_bf16<FMT>(vr[s].x, vr[s].y);
-      vf[2 * s + 1] = codes_bf16<FMT>(vr[s].z, vr[s].w);
+      for (int s = 0; s < S; ++s) {
+        vf[2 * s] = codes_bf16<FMT>(vr[s].x, vr[s].y);
+        vf[2 * s + 1] = codes_bf16<FMT>(vr[s].z, vr[s].w);
+      }
     }
-    // the next page's loads are in flight during the rest
     if (it + 1 < npages) {
       if (((it + 1) & 63) == 0) fetch_ids(it + 1);
-      load(it + 1);
+      load_keys(it + 1);
+      if constexpr (RPW == 1) load_values();
     }
     bf16x8 pf[RPW][Row::PP];
     page_softmax<MASKED>(row, sc, ks, vs, tree, page * kPage - t.L, t.node0, masks, lg, pf);
 #pragma unroll
-    for (int d = 0; d < DT; d += 2) value_step(row, d, vf[d], vf[d + 1], pf);
+    for (int d = 0; d < DT; d += 2) {
+      if constexpr (RPW == 1) {
+        value_step(row, d, vf[d], vf[d + 1], pf);
+      } else {
+        const u32x4 w = vr[d / 2];
+        value_step(row, d, codes_bf16<FMT>(w.x, w.y), codes_bf16<FMT>(w.z, w.w), pf);
+      }
+    }
+    if constexpr (RPW > 1) {
+      if (it + 1 < npages) load_values();
+    }
+    bad = next_bad;
   };
   // the pages of prompt tokens only, then those that hold nodes
   const int plain = min(npages, max(0, (t.L / kPage - t.beg - kw + KW - 1) / KW));
-  if (npages > 0) load(0);
+  if (npages > 0) {
+    load_keys(0);
+    load_values();
+    bad = next_bad;
+  }
   int it = 0;
   for (; it < plain; ++it) step(std::false_type{}, it);
   for (; it < npages; ++it) step(std::true_type{}, it);

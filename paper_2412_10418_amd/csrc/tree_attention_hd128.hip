@@ -10,26 +10,32 @@ hipError_t tree_attn_hd128(const TreeAttnArgs& a, const TreeAttnPlan& p, int dty
   return tree_attn_hd<128>(a, p, dtype, st);
 }
 
-TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, int dtype) {
+TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len) {
   TreeAttnPlan p{};
   const int tiles = (int)(((long long)n * (H / Hkv) + 15) / 16);
   p.few = tiles <= 2 ? tiles : 0;
-  // Two row tiles a wave read every fragment of a page once for both: better
-  // where the LDS and the vector units bound it (bf16, 16 prompt x KV head
-  // pairs of 128 tiles: 78 against 95 us).  In fp32 the matrix units have
-  // twice the work and more waves hide more (512 pairs of 17 tiles: 279
-  // against 310 us).
-  p.rpw = dtype == 1 && tiles > 4 ? 2 : 1;
+  // Two row tiles a wave read every fragment of a page once for both, and take
+  // 0.93 of the time a tile where they fill the chip (64 prompts x 8 KV heads
+  // of 16 tiles at 1024 tokens: 181 against 190 us in fp32, 116 against 130 in
+  // bf16); not where they leave slots empty (17 tiles: 237 against 218) or
+  // give less than three workgroups a CU (16 pairs of 128 tiles: 105 against
+  // 87).
+  const long long pairs = (long long)B * Hkv;
+  const long long one = (tiles + 3) / 4, two = (tiles + 7) / 8;
+  p.rpw = !p.few && pairs * two >= 768 && 8 * two * 0.93 < 4 * one ? 2 : 1;
   const int most_tiles = p.few ? p.few : 4 * p.rpw;
   p.row_groups = (tiles + most_tiles - 1) / most_tiles;
   p.wg_tiles = (tiles + p.row_groups - 1) / p.row_groups;
-  // Keys are split until there are two workgroups a CU, counted in groups of
-  // four tiles whatever the type; a split has four pages (few rows: eight, two
-  // a wave) at least.
-  const long long wgs = (long long)B * Hkv * (p.few ? 1 : (tiles + 3) / 4);
+  // Keys are split until there are two workgroups a CU; a split has eight pages
+  // (few rows: two a wave) or four at least.  More and smaller splits start
+  // more often than they balance (32 prompts of one token at 4096: 39 us at
+  // 512 workgroups, 43 at 1024, 51 at 2048).
+  const long long wgs = pairs * (p.few ? 1 : one);
   const long long pages = ((long long)max_len + n + kPage - 1) / kPage;
   const long long most = std::max<long long>(1, pages / (p.few ? 8 : 4));
-  p.nsplit = (int)std::min<long long>({std::max<long long>(1, 512 / std::max<long long>(wgs, 1)), most, kTreeMaxSplits});
+  const long long want = std::max<long long>(1, 512 / std::max<long long>(wgs, 1));
+  p.nsplit = (int)std::min<long long>({want, most, kTreeMaxSplits});
+  p.split_pages = (int)std::min<long long>((pages + p.nsplit - 1) / p.nsplit, 1 << 26);
   p.workspace = p.nsplit > 1 ? (size_t)p.nsplit * B * n * H * (hd + 2) * sizeof(float) : 0;
   return p;
 }
@@ -38,6 +44,7 @@ hipError_t tree_attn_launch(TreeAttnArgs a, const TreeAttnPlan& p, int dtype, vo
   if (a.c.B == 0 || a.n == 0) return hipSuccess;
   a.nsplit = p.nsplit;
   a.row_groups = p.row_groups;
+  a.split_pages = p.nsplit > 1 ? p.split_pages : 0;
   a.wg_tiles = p.wg_tiles;
   a.part_o = (float*)workspace;
   a.part_ml = a.part_o + (size_t)p.nsplit * a.c.B * a.n * a.H * a.c.hd;
