@@ -238,14 +238,18 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q,
  * on (path[b][0] = 0), the rest of path [batch][n] is -1.  n_nodes (NULL: n)
  * is clamped to 1..n.  A child whose token is outside [0, V), or whose parent
  * is outside [0, j), is passed over.  u [batch][n] and v [batch] are uniforms
- * in [0, 1).  Errors: EINVAL, ERANGE (n beyond CDSL_TREE_MAX, V beyond
- * CDSL_ACCEPT_MAX_VOCAB), EDEVICE. */
+ * in [0, 1).  The workspace must hold cdsl_op_tree_accept_workspace bytes (0:
+ * none needed); it needs no initial contents.  Errors: EINVAL, ERANGE (batch
+ * beyond 65535, n beyond CDSL_TREE_MAX, V beyond CDSL_ACCEPT_MAX_VOCAB),
+ * EDEVICE. */
+size_t cdsl_op_tree_accept_workspace(int32_t batch, int32_t n, int32_t V);
 int cdsl_op_tree_accept(const float* target_probs, const float* draft_probs,
                         int32_t batch, int32_t n, int32_t V,
                         const int32_t* tokens, const int32_t* parents,
                         const int32_t* n_nodes, const float* u, const float* v,
                         int32_t replace, int32_t* path, int32_t* n_path,
-                        int32_t* next_token, void* stream);
+                        int32_t* next_token, void* workspace,
+                        size_t workspace_bytes, void* stream);
 
 /* Keeps a path of each prompt's tree: in every layer, the entry at position
  * lens[b] + path[b][i] moves to lens[b] + i, i < n_path[b] (clamped to

@@ -35,7 +35,8 @@ EXPORTS = [
     "cdsl_free_prefix", "cdsl_destroy", "cdsl_last_error", "cdsl_profile_enable", "cdsl_profile_read",
     "cdsl_op_gemm_workspace", "cdsl_op_gemm", "cdsl_op_gemm_static", "cdsl_op_logit_rows",
     "cdsl_op_kvq_pool_bytes", "cdsl_op_kvq_write", "cdsl_op_kvq_read", "cdsl_op_kvq_keep",
-    "cdsl_op_tree_attention_workspace", "cdsl_op_tree_attention", "cdsl_op_tree_accept",
+    "cdsl_op_tree_attention_workspace", "cdsl_op_tree_attention", "cdsl_op_tree_accept_workspace",
+    "cdsl_op_tree_accept",
 ]
 
 
@@ -135,7 +136,8 @@ def lib():
         "cdsl_op_tree_attention_workspace": ([i32, i32, i32, i32, i32, i32], C.c_size_t),
         "cdsl_op_tree_attention": ([vp, i32, vp, i32, i32, i32, i64, i64, vp, vp, vp, f32, i32, vp, vp, C.c_size_t,
                                     vp], i32),
-        "cdsl_op_tree_accept": ([vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp], i32),
+        "cdsl_op_tree_accept_workspace": ([i32, i32, i32], C.c_size_t),
+        "cdsl_op_tree_accept": ([vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, C.c_size_t, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -427,11 +429,15 @@ def cdsl_op_tree_accept(target_probs: torch.Tensor, draft_probs: torch.Tensor, t
     out = torch.empty(B * (n + 2), dtype=torch.int32, device=target_probs.device)
     path, n_path, token = out[:B * n].view(B, n), out[B * n:B * n + B], out[B * n + B:]
     at = out.data_ptr()
-    _call(dev, lib().cdsl_op_tree_accept, _of(target_probs, shape, torch.float32, dev, "target_probs"),
+    L = lib()
+    need = L.cdsl_op_tree_accept_workspace(B, n, V)
+    ws = torch.empty(need, dtype=torch.uint8, device=out.device) if need else None
+    _call(dev, L.cdsl_op_tree_accept, _of(target_probs, shape, torch.float32, dev, "target_probs"),
           _of(draft_probs, shape, torch.float32, dev, "draft_probs"), B, n, V,
           _of(tokens, (B, n), torch.int32, dev, "tokens"), _of(parents, (B, n), torch.int32, dev, "parents"),
           _ints(n_nodes, (B,), dev, "n_nodes"), _of(u, (B, n), torch.float32, dev, "u"),
-          _of(v, (B,), torch.float32, dev, "v"), 1 if replace else 0, at, at + 4 * B * n, at + 4 * B * (n + 1))
+          _of(v, (B,), torch.float32, dev, "v"), 1 if replace else 0, at, at + 4 * B * n, at + 4 * B * (n + 1),
+          ws.data_ptr() if need else None, need)
     return path, n_path, token
 
 

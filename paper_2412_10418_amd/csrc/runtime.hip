@@ -2004,10 +2004,15 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, 
   });
 }
 
+size_t cdsl_op_tree_accept_workspace(int32_t batch, int32_t n, int32_t V) {
+  if (batch <= 0 || n <= 0 || n > CDSL_TREE_MAX || V <= 0 || V > CDSL_ACCEPT_MAX_VOCAB) return 0;
+  return tree_accept_workspace(batch, n, V);
+}
+
 int cdsl_op_tree_accept(const float* target_probs, const float* draft_probs, int32_t batch, int32_t n, int32_t V,
                         const int32_t* tokens, const int32_t* parents, const int32_t* n_nodes, const float* u,
                         const float* v, int32_t replace, int32_t* path, int32_t* n_path, int32_t* next_token,
-                        void* stream) {
+                        void* workspace, size_t workspace_bytes, void* stream) {
   return guarded(nullptr, [&]() -> int {
     if ((!target_probs || !draft_probs || !tokens || !parents || !u || !v || !path || !n_path || !next_token) &&
         batch != 0)
@@ -2015,8 +2020,12 @@ int cdsl_op_tree_accept(const float* target_probs, const float* draft_probs, int
     if (batch < 0 || n <= 0 || V <= 0) return fail(nullptr, CDSL_EINVAL, "bad sizes");
     if (n > CDSL_TREE_MAX) return fail(nullptr, CDSL_ERANGE, "a tree has at most 512 nodes");
     if (V > CDSL_ACCEPT_MAX_VOCAB) return fail(nullptr, CDSL_ERANGE, "vocabulary beyond 2^20");
+    if (batch > 65535) return fail(nullptr, CDSL_ERANGE, "more than 65535 prompts");
+    const size_t need = batch > 0 ? tree_accept_workspace(batch, n, V) : 0;
+    if (need > 0 && (!workspace || workspace_bytes < need)) return fail(nullptr, CDSL_EINVAL, "workspace too small");
+    if (!aligned16(workspace)) return fail(nullptr, CDSL_EINVAL, "the workspace must be 16-byte aligned");
     return launched(tree_accept_launch(target_probs, draft_probs, batch, n, V, tokens, parents, n_nodes, u, v,
-                                       replace, path, n_path, next_token, (hipStream_t)stream));
+                                       replace, path, n_path, next_token, workspace, (hipStream_t)stream));
   });
 }
 

@@ -54,8 +54,9 @@ hipError_t tree_attn_launch(TreeAttnArgs a, const TreeAttnPlan& p, int dtype, vo
 
 constexpr int kAcceptMaxVocab = 1 << 20;
 
+size_t tree_accept_workspace(int B, int n, int V);
 hipError_t tree_accept_launch(const float* p, const float* q, int B, int n, int V, const int* tokens,
                               const int* parents, const int* n_nodes, const float* u, const float* v, int replace,
-                              int* path, int* n_path, int* next_token, hipStream_t st);
+                              int* path, int* n_path, int* next_token, void* workspace, hipStream_t st);
 
 }  // namespace cdsl

@@ -17,22 +17,29 @@
 // draw among 32000 flat entries would land next to its token once in about
 // thirty.
 //
-// One workgroup per prompt: the walk is a chain of decisions, and only the
-// rows it rejects at, and the last one, are read.  The probabilities of all
-// children are fetched at once first, so that the walk itself stays in LDS.
-// Latency bounds it, so a row's loads are all in flight together, and rows of
-// up to 32768 ids stay in registers for the node's further sums and the draw.
+// The walk is a chain of decisions, and only the rows it rejects at, and the
+// last one, are read.  The probabilities of all children are fetched at once
+// first, so that the walk itself stays in LDS.  Latency bounds it, and the
+// fp64 rate of one CU (3 us for a sum over 32000 ids, 13 us over 128256).  Rows
+// of up to 32768 ids: one workgroup per prompt, which keeps a node's rows in
+// its registers for the node's further sums and the draw.  Longer rows: the
+// first kRounds sums have a launch each, with a workgroup per chunk of the
+// row; each of them walks to the next sum that is needed, from where the
+// launch before stopped, and a last launch, one workgroup per prompt, adds up
+// what is left and draws.
 #include "tree.h"
 
 namespace cdsl {
 
 namespace {
 
+struct At;
 constexpr int NT = 1024, NW = NT / 64;
 constexpr int RUN = 1024;                       // consecutive ids of a wave in a chunk: 16 a lane
 constexpr int CHUNK = NW * RUN;
 constexpr int kSegs = kAcceptMaxVocab / RUN;    // (chunk, wave) sums at most
 constexpr int kHeld = 2;                        // chunks that registers hold
+constexpr int kRounds = 4;                      // sums of a long row that have a launch of their own
 
 // Sum over a wave, the same bits in every lane: rotations within rows of 16,
 // then swaps of rows and halves (a shuffle through LDS takes five times as long).
@@ -97,50 +104,213 @@ __device__ __forceinline__ double weights(const Piece& p, const Piece& q, double
   return 0.5 * (d + a);
 }
 
-// HELD: V <= kHeld * CHUNK.
+struct AcceptArgs {
+  const float* p;
+  const float* q;
+  int n, V;
+  const int* tokens;
+  const int* parents;
+  const int* n_nodes;
+  const float* u;
+  const float* v;
+  int replace;
+  int* path;
+  int* n_path;
+  int* next_token;
+  // long rows: what the launches hand on (see tree_accept_workspace)
+  At* at;           // [kRounds][B]: where a round's walk stopped
+  double* parts;           // [kRounds][B][segs]: the sums of runs that it stopped for
+  float* kids;             // [2][B][n]: the children's p and q
+  long long kid_stride;    // B * n
+  int round;               // rounds before this launch
+};
+
+// A prompt's tree in LDS, and the state of its walk; alike in every wave.
+struct Walk {
+  int par[kTreeMax], tok[kTreeMax];
+  float px[kTreeMax], qx[kTreeMax], us[kTreeMax];
+};
+struct At {
+  int cur = 0, len = 1, from = 1;
+  int none = 0;            // no mass left
+  int summed = 0;          // N is the sum of the present c
+  int fell = -1;           // the child that is being rejected (stopped for its sum)
+  int over = 0;            // walked, and summed
+  double c = 0., N = 1., rest = 1.;
+};
+
+// First launch: the children's probabilities come from their rows, and later
+// launches find them in a.kids.
+template <bool FIRST>
+__device__ __forceinline__ void fetch_tree(const AcceptArgs& a, int b, int nb, bool keep, Walk& w) {
+  const long long row0 = (long long)b * a.n;
+  for (int j = threadIdx.x; j < nb; j += NT) {
+    int c = j > 0 ? a.parents[row0 + j] : -1;
+    const int x = a.tokens[row0 + j];
+    const float uj = a.u[row0 + j];
+    float* kp = a.kids + row0 + j;
+    float* kq = kp + a.kid_stride;
+    float pj = 0.f, qj = 0.f;
+    if constexpr (!FIRST) pj = *kp, qj = *kq;
+    if (c < 0 || c >= j || x < 0 || x >= a.V) c = -1;   // not a child that can be taken
+    if (FIRST && c >= 0) {
+      pj = a.p[(row0 + c) * a.V + x];
+      qj = a.q[(row0 + c) * a.V + x];
+    }
+    if (FIRST && keep) *kp = pj, *kq = qj;
+    w.par[j] = c;
+    w.tok[j] = x;
+    w.px[j] = pj;
+    w.qx[j] = qj;
+    w.us[j] = uj;
+  }
+  __syncthreads();
+}
+
+// What follows a sum (at.N, for at.c).
+__device__ __forceinline__ void walk_summed(const AcceptArgs& a, const Walk& w, At& at) {
+  const int lane = threadIdx.x & 63, fell = at.fell;
+  at.fell = -1;
+  at.summed = 1;
+  if (fell < 0) {
+    at.over = 1;
+    return;
+  }
+  if (!a.replace) {
+    // a token that an earlier sibling carried is out of q already
+    bool twice = false;
+    for (int s = 0; s < fell; s += 64) {
+      const int e = s + lane;
+      twice = twice || __ballot(e < fell && w.par[e] == at.cur && w.tok[e] == w.tok[fell]);
+    }
+    if (!twice) at.rest -= (double)w.qx[fell];
+  }
+  if (!(at.N > 0.)) at.none = 1;
+}
+
+// Walks to the next sum that is needed, for at.c; false: none is (at.over).
+// moved(node, place on the path): a node is reached.
+template <typename Moved>
+__device__ __forceinline__ bool walk_on(const Walk& w, int nb, At& at, Moved&& moved) {
+  const int lane = threadIdx.x & 63;
+  if (at.over) return false;
+  int fell = -1;   // the child that is rejected next
+  while (at.from < nb && !at.none && fell < 0) {   // 64 nodes at a time
+    const int j0 = at.from & ~63, j = j0 + lane;
+    const unsigned long long kids = __ballot(j >= at.from && j < nb && w.par[j] == at.cur);
+    if (!kids) {
+      at.from = j0 + 64;
+      continue;
+    }
+    const int k = j0 + __builtin_ctzll(kids);
+    at.from = k + 1;
+    if (!(at.rest > 0.)) continue;
+    const double pk = at.c > 0. ? weight(w.px[k], w.qx[k], at.c) / at.N : (double)w.px[k];
+    const double qk = (double)w.qx[k] / at.rest;
+    if (pk > 0. && (double)w.us[k] * qk <= pk) {
+      moved(k, at.len);
+      ++at.len;
+      at.cur = k;
+      at.c = 0., at.N = 1., at.rest = 1.;
+      at.summed = 0;
+    } else {
+      fell = k;
+    }
+  }
+  if (fell < 0 && at.summed) {
+    at.over = 1;
+    return false;
+  }
+  at.fell = fell;
+  if (fell >= 0) at.c += at.N / at.rest;
+  return true;
+}
+
+// Sum of the parts of a row, in every lane.
+__device__ __forceinline__ double sum_parts(const double* part, int segs) {
+  double t = 0.;
+  for (int k = threadIdx.x & 63; k < segs; k += 64) t += part[k];
+  return wave_sum_d(t);
+}
+
+// The state after the rounds before this launch: where the last one stopped,
+// with the sum that it stopped for.  (Loaded before the tree, so that their
+// latencies overlap; the parts of a prompt that is over are not used.)
+__device__ __forceinline__ At stopped(const AcceptArgs& a, int b, int B, int segs) {
+  At at;
+  if (a.round > 0) {
+    const long long slot = (long long)(a.round - 1) * B + b;
+    const double* part = a.parts + slot * segs;
+    double t = 0.;
+    for (int k = threadIdx.x & 63; k < segs; k += 64) t += part[k];
+    at = a.at[slot];
+    if (!at.over) at.N = wave_sum_d(t);
+  }
+  return at;
+}
+
+// One round: the walk to the next sum, and the sums of this chunk's runs for
+// it.  Workgroup = (chunk, prompt); the first of a prompt hands the state on.
+template <bool FIRST>
+__global__ __launch_bounds__(NT) void tree_sums_kernel(AcceptArgs a) {
+  __shared__ Walk w;
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int nb = a.n_nodes ? min(max(a.n_nodes[b], 1), a.n) : a.n;
+  const int segs = gridDim.x * NW;
+  const bool lead = blockIdx.x == 0 && tid == 0;
+  const long long row0 = (long long)b * a.n;
+  At at = stopped(a, b, gridDim.y, segs);
+  fetch_tree<FIRST>(a, b, nb, blockIdx.x == 0, w);
+  if (!FIRST && !at.over) walk_summed(a, w, at);
+  const bool need = walk_on(w, nb, at, [&](int k, int place) {
+    if (lead) a.path[row0 + place] = k;
+  });
+  const long long slot = (long long)a.round * gridDim.y + b;
+  if (lead) a.at[slot] = at;
+  if (!need) return;
+  const long long row = (row0 + at.cur) * a.V;
+  const int i = CHUNK * blockIdx.x + wv * RUN + 4 * lane;
+  Piece p, q{};
+  p.load(a.p + row, i, a.V);
+  if (at.c > 0.) q.load(a.q + row, i, a.V);
+  const double s = wave_sum_d(weights(p, q, at.c));
+  if (lane == 0) a.parts[slot * segs + blockIdx.x * NW + wv] = s;
+}
+
+// HELD: V <= kHeld * CHUNK, the one launch; else the one after the rounds.
 template <bool HELD>
-__global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict__ p_all,
-                                                         const float* __restrict__ q_all, int n, int V,
-                                                         const int* __restrict__ tokens,
-                                                         const int* __restrict__ parents,
-                                                         const int* __restrict__ n_nodes, const float* __restrict__ u,
-                                                         const float* __restrict__ v, int replace, int* path,
-                                                         int* n_path, int* next_token) {
-  __shared__ int par[kTreeMax], tok[kTreeMax], walk[kTreeMax];
-  __shared__ float px[kTreeMax], qx[kTreeMax], us[kTreeMax];
+__global__ __launch_bounds__(NT) void tree_accept_kernel(AcceptArgs a) {
+  __shared__ Walk w;
   __shared__ double part[HELD ? kHeld * NW : kSegs];
   __shared__ int hit, best_i[NW];
   __shared__ float best_v[NW];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int nb = n_nodes ? min(max(n_nodes[b], 1), n) : n;
-  const long long row0 = (long long)b * n;
-  for (int j = tid; j < nb; j += NT) {
-    int c = j > 0 ? parents[row0 + j] : -1;
-    const int x = tokens[row0 + j];
-    const float uj = u[row0 + j];
-    if (c < 0 || c >= j || x < 0 || x >= V) c = -1;   // not a child that can be taken
-    par[j] = c;
-    tok[j] = x;
-    if (c >= 0) {
-      px[j] = p_all[(row0 + c) * V + x];
-      qx[j] = q_all[(row0 + c) * V + x];
-      us[j] = uj;
-    }
-  }
-  if (tid == 0) walk[0] = 0, hit = -1;
-  __syncthreads();
-
+  const int b = blockIdx.x, V = a.V, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int nb = a.n_nodes ? min(max(a.n_nodes[b], 1), a.n) : a.n;
+  const long long row0 = (long long)b * a.n;
+  if (tid == 0) hit = -1;
   const int chunks = (V + CHUNK - 1) / CHUNK, segs = chunks * NW;
+  At at = stopped(a, b, gridDim.x, segs);
+  fetch_tree<HELD>(a, b, nb, false, w);
   const int at0 = wv * RUN + 4 * lane;   // this lane's first id of a chunk
-  int cur = 0, len = 1, from = 1;
-  double c = 0., N = 1., rest = 1.;
-  const float* p = p_all + row0 * V;
-  const float* q = q_all + row0 * V;
+  bool known = false;      // the parts that at.N is the sum of are in a.parts
+  if constexpr (!HELD) {
+    if (!at.over) walk_summed(a, w, at);
+    known = true;
+  }
+  const float* p = a.p + (row0 + at.cur) * V;
+  const float* q = a.q + (row0 + at.cur) * V;
   Piece hp[HELD ? kHeld : 1], hq[HELD ? kHeld : 1];
-  bool have_p = false, have_q = false;   // the held pieces are those of cur
+  bool have_p = false, have_q = false;   // the held pieces are those of the node reached
 
-  // part[chunk * NW + wave] and their sum, for the present c
-  auto sum = [&]() __attribute__((always_inline)) -> double {
+  while (walk_on(w, nb, at, [&](int k, int place) {
+    if (tid == 0) a.path[row0 + place] = k;
+    p = a.p + (row0 + k) * V;
+    q = a.q + (row0 + k) * V;
+    have_p = have_q = false;
+  })) {
+    // part[chunk * NW + wave] and their sum, for the present c
+    const double c = at.c;
+    known = false;
     __syncthreads();   // earlier readers of part are done
     if constexpr (HELD) {
       const bool lp = !have_p, lq = !have_q && c > 0.;
@@ -176,59 +346,21 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict
       }
     }
     __syncthreads();
-    double t = 0.;
-    for (int k = lane; k < segs; k += 64) t += part[k];
-    return wave_sum_d(t);
-  };
-
-  // Every wave walks alike, 64 nodes at a time, from one sum to the next.
-  bool none = false, done = false, summed = false;   // no mass left; walked; part holds the sums of the present c
-  while (true) {
-    int fell = -1;   // the child that is rejected next
-    while (from < nb && !none && fell < 0) {
-      const int j0 = from & ~63, j = j0 + lane;
-      const unsigned long long kids = __ballot(j >= from && j < nb && par[j] == cur);
-      if (!kids) {
-        from = j0 + 64;
-        continue;
-      }
-      const int k = j0 + __builtin_ctzll(kids);
-      from = k + 1;
-      if (!(rest > 0.)) continue;
-      const double pk = c > 0. ? weight(px[k], qx[k], c) / N : (double)px[k];
-      const double qk = (double)qx[k] / rest;
-      if (pk > 0. && (double)us[k] * qk <= pk) {
-        if (tid == 0) walk[len] = k;
-        ++len;
-        cur = k;
-        p = p_all + (row0 + k) * V;
-        q = q_all + (row0 + k) * V;
-        c = 0., N = 1., rest = 1.;
-        summed = have_p = have_q = false;
-      } else {
-        fell = k;
-      }
-    }
-    done = fell < 0;
-    if (!done) c += N / rest;
-    if (done && summed) break;
-    N = sum();
-    if (done) break;
-    summed = true;
-    if (!replace) {
-      // a token that an earlier sibling carried is out of q already
-      bool twice = false;
-      for (int s = 0; s < fell; s += 64) {
-        const int e = s + lane;
-        twice = twice || __ballot(e < fell && par[e] == cur && tok[e] == tok[fell]);
-      }
-      if (!twice) rest -= (double)qx[fell];
-    }
-    if (!(N > 0.)) none = true;
+    at.N = sum_parts(part, segs);
+    walk_summed(a, w, at);
+  }
+  if (!HELD && known) {
+    // they are the last ones that a round stopped for (the first round always does)
+    int r = a.round - 1;
+    while (r > 0 && a.at[(long long)r * gridDim.x + b].over) --r;
+    const double* from = a.parts + ((long long)r * gridDim.x + b) * segs;
+    for (int k = tid; k < segs; k += NT) part[k] = from[k];
+    __syncthreads();
   }
 
   // The draw: the first id whose running sum passes v * (sum).
-  if (none) {
+  const double c = at.c, N = at.N;
+  if (at.none) {
     // argmax p, lowest id on ties
     float bv = -INFINITY;
     int bi = 0;
@@ -249,10 +381,10 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict
       hit = N == 0. ? bi : -1;
     }
   } else if (N > 0. && N < INFINITY) {
-    // first entry of a row of lanes whose running sum from `at` passes T (the
+    // first entry of a row of lanes whose running sum from `sum_at` passes T (the
     // last one with mass when rounding leaves T past the total), and the sum
     // before it
-    auto locate = [&](double mine, double T, double& at) __attribute__((always_inline)) -> int {
+    auto locate = [&](double mine, double T, double& sum_at) __attribute__((always_inline)) -> int {
       double incl = mine;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -261,26 +393,26 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict
       }
       double before = __shfl_up(incl, 1, 64);
       if (lane == 0) before = 0.;
-      const unsigned long long past = __ballot(mine > 0. && at + incl > T), mass = __ballot(mine > 0.);
+      const unsigned long long past = __ballot(mine > 0. && sum_at + incl > T), mass = __ballot(mine > 0.);
       const int src = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(mass | 1ull);
-      at += __shfl(before, src, 64);
+      sum_at += __shfl(before, src, 64);
       return mass ? src : -1;
     };
-    const double T = (double)v[b] * N;
+    const double T = (double)a.v[b] * N;
     // each lane takes a run of segments
     const int run = (segs + 63) / 64;
-    double mine = 0., at = 0.;
+    double mine = 0., from = 0.;
     for (int s = lane * run; s < min(segs, lane * run + run); ++s) mine += part[s];
-    const int src = locate(mine, T, at);
+    const int src = locate(mine, T, from);
     int seg = -1;
-    double seg_at = at;
+    double seg_at = from;
     for (int s = src * run; src >= 0 && s < min(segs, src * run + run); ++s) {
       if (part[s] > 0.) {
         seg = s;
-        seg_at = at;
-        if (at + part[s] > T) break;
+        seg_at = from;
+        if (from + part[s] > T) break;
       }
-      at += part[s];
+      from += part[s];
     }
     if (seg >= 0 && wv == seg % NW) {   // its wave: 4 x 64 lanes x 4 ids in order
       const int i0 = CHUNK * (seg / NW) + at0;
@@ -323,25 +455,70 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(const float* __restrict
     }
   }
   __syncthreads();
-  for (int i = tid; i < n; i += NT) path[row0 + i] = i < len ? walk[i] : -1;
+  for (int i = at.len + tid; i < a.n; i += NT) a.path[row0 + i] = -1;
   if (tid == 0) {
-    n_path[b] = len;
-    next_token[b] = hit;
+    a.path[row0] = 0;
+    a.n_path[b] = at.len;
+    a.next_token[b] = hit;
   }
 }
 
+int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
+
 }  // namespace
+
+namespace {
+struct AcceptWs {
+  size_t parts, kids, total;   // the states come first
+};
+AcceptWs accept_ws(int B, int n, int V) {
+  auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  AcceptWs w{};
+  if (V <= kHeld * CHUNK) return w;
+  w.parts = al(sizeof(At) * kRounds * B);
+  w.kids = w.parts + al((size_t)kRounds * B * chunks_of(V) * NW * sizeof(double));
+  w.total = w.kids + (size_t)2 * B * n * sizeof(float);
+  return w;
+}
+}  // namespace
+
+size_t tree_accept_workspace(int B, int n, int V) { return accept_ws(B, n, V).total; }
 
 hipError_t tree_accept_launch(const float* p, const float* q, int B, int n, int V, const int* tokens,
                               const int* parents, const int* n_nodes, const float* u, const float* v, int replace,
-                              int* path, int* n_path, int* next_token, hipStream_t st) {
+                              int* path, int* n_path, int* next_token, void* workspace, hipStream_t st) {
   if (B == 0) return hipSuccess;
-  if (V <= kHeld * CHUNK)
-    tree_accept_kernel<true><<<B, NT, 0, st>>>(p, q, n, V, tokens, parents, n_nodes, u, v, replace, path, n_path,
-                                               next_token);
-  else
-    tree_accept_kernel<false><<<B, NT, 0, st>>>(p, q, n, V, tokens, parents, n_nodes, u, v, replace, path, n_path,
-                                                next_token);
+  AcceptArgs a{};
+  a.p = p;
+  a.q = q;
+  a.n = n;
+  a.V = V;
+  a.tokens = tokens;
+  a.parents = parents;
+  a.n_nodes = n_nodes;
+  a.u = u;
+  a.v = v;
+  a.replace = replace;
+  a.path = path;
+  a.n_path = n_path;
+  a.next_token = next_token;
+  a.kid_stride = (long long)B * n;
+  if (V <= kHeld * CHUNK) {
+    tree_accept_kernel<true><<<B, NT, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  const AcceptWs ws = accept_ws(B, n, V);
+  a.at = (At*)workspace;
+  a.parts = (double*)((char*)workspace + ws.parts);
+  a.kids = (float*)((char*)workspace + ws.kids);
+  const dim3 grid((unsigned)chunks_of(V), (unsigned)B);
+  for (; a.round < kRounds; ++a.round) {
+    if (a.round == 0) tree_sums_kernel<true><<<grid, NT, 0, st>>>(a);
+    else tree_sums_kernel<false><<<grid, NT, 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  tree_accept_kernel<false><<<B, NT, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -35,8 +35,10 @@ def _attend(c, layer=0, Q=P, dtype=0, n=4, H=8, qsb=2048, qst=512, lens=P, paren
                  parents, scale, max_len, out, ws, ws_bytes, None)
 
 
-def _accept(p=P, q=P, B=2, n=4, V=100, tokens=P, parents=P, u=P, v=P, path=P, n_path=P, token=P):
-    return _call("cdsl_op_tree_accept", p, q, B, n, V, tokens, parents, None, u, v, 1, path, n_path, token, None)
+def _accept(p=P, q=P, B=2, n=4, V=100, tokens=P, parents=P, u=P, v=P, path=P, n_path=P, token=P, ws=None,
+            ws_bytes=0):
+    return _call("cdsl_op_tree_accept", p, q, B, n, V, tokens, parents, None, u, v, 1, path, n_path, token, ws, ws_bytes,
+                 None)
 
 
 def _keep(c, lens=P, path=P, n_path=P, n=4, new=P + 64):
@@ -103,6 +105,15 @@ def test_trees_that_cannot_be_verified():
         assert _accept(**kw) == CDSL_EINVAL, kw
     assert _accept(n=513) == CDSL_ERANGE
     assert _accept(V=(1 << 20) + 1) == CDSL_ERANGE
+    assert _accept(B=65536) == CDSL_ERANGE
+    # long rows need their workspace
+    from paper_2412_10418_amd import binding as bd
+    need = bd.lib().cdsl_op_tree_accept_workspace(2, 4, 128256)
+    assert need > 0 and bd.lib().cdsl_op_tree_accept_workspace(2, 4, 32000) == 0
+    for ws, size in ((None, 0), (P, need - 1), (None, need), (P + 8, need)):
+        assert _accept(V=128256, ws=ws, ws_bytes=size) == CDSL_EINVAL
+    for bad in ((0, 4, 128256), (2, 0, 128256), (2, 513, 128256), (2, 4, 0), (2, 4, (1 << 20) + 1)):
+        assert bd.lib().cdsl_op_tree_accept_workspace(*bad) == 0
 
 
 def test_paths_that_cannot_be_kept():
