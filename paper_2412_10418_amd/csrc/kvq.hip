@@ -94,6 +94,32 @@ __device__ __forceinline__ void transpose4(const unsigned (&w)[4], unsigned (&o)
   o[3] = __builtin_amdgcn_perm(d, c, 0x07060302);
 }
 
+// Maximum over groups of LANES lanes (8, 16 or 32): within quads, halves of a
+// row, rows of 16, then the two rows; vector instructions only (shuffles
+// through LDS, 40 a thread, took 6 us of 42 at 24 prompts of up to 2047).
+template <int CTRL>
+__device__ __forceinline__ unsigned max_moved(unsigned a) {
+  return max(a, (unsigned)__builtin_amdgcn_update_dpp(0, (int)a, CTRL, 0xf, 0xf, false));
+}
+template <int LANES>
+__device__ __forceinline__ unsigned group_max(unsigned a) {
+  a = max_moved<0xB1>(a);                             // quad_perm 1 0 3 2
+  a = max_moved<0x4E>(a);                             // quad_perm 2 3 0 1
+  a = max_moved<0x141>(a);                            // row_half_mirror
+  if constexpr (LANES > 8) a = max_moved<0x140>(a);   // row_mirror
+  if constexpr (LANES > 16) {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 t = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    a = max(t.x, t.y);
+  }
+  return a;
+}
+
+// Where word w of a unit's codes stands in LDS: the sixteen 16-byte chunks of a
+// row of 64 words are permuted by the row, so that neither the order of the
+// rows (dims along the lanes) nor that of the unit meets one bank often.
+__device__ __forceinline__ int banked(int w) { return w ^ ((w >> 6 & 15) << 2); }
+
 // Threads of a workgroup: a task is four slots x four dims of the keys or of
 // the values (16 hd / 4 tasks a unit), so that a quarter-row load or store of
 // the fp32 or bf16 side is contiguous over the lanes and a task's 4 x 4 codes
@@ -144,8 +170,7 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_write_kernel(KvqView c,
       unsigned a = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) a = max(a, __float_as_uint(x[u][t][e]) & 0x7fffffffu);
-#pragma unroll
-      for (int o = LQ / 2; o > 0; o >>= 1) a = max(a, (unsigned)__shfl_xor((int)a, o, 64));
+      a = group_max<LQ>(a);
       const bool bad = a >= 0x7f800000u;
       s[t] = bad ? __uint_as_float(0x7fc00000u) : scale_of<FMT>(__uint_as_float(a));
       w[t] = bad ? 0u : encode4<FMT>(x[u][t], s[t]);
@@ -164,8 +189,8 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_write_kernel(KvqView c,
     if (whole) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        if (isv) lds[kvq_value_at(HD, slot, d + t) / 4] = o[t];
-        else lds[kvq_key_at(slot + t, d) / 4] = w[t];
+        if (isv) lds[banked(kvq_value_at(HD, slot, d + t) / 4)] = o[t];
+        else lds[banked(kvq_key_at(slot + t, d) / 4)] = w[t];
       }
     } else {
 #pragma unroll
@@ -182,7 +207,7 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_write_kernel(KvqView c,
   if (!whole) return;   // uniform over the workgroup
   __syncthreads();
 #pragma unroll
-  for (int i = threadIdx.x; i < 2 * kPage * HD / 16; i += NT) *((u32x4*)unit + i) = *((const u32x4*)lds + i);
+  for (int i = threadIdx.x; i < 2 * kPage * HD / 16; i += NT) *((u32x4*)unit + i) = *(const u32x4*)&lds[banked(4 * i)];
 }
 
 // Workgroup = (page of the prompt's run, KV head, prompt): the unit comes in
@@ -193,7 +218,7 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_read_kernel(KvqView c, 
   constexpr int NT = kvq_threads<HD>();
   constexpr int LQ = HD / 4;
   constexpr int PER = 4 * HD / NT;
-  constexpr int WORDS = kvq_unit_bytes(HD) / 4;
+  constexpr int WORDS = kvq_unit_bytes(HD) / 4, CODES = 2 * kPage * HD / 4;
   __shared__ __attribute__((aligned(16))) unsigned lds[WORDS];
   const int b = blockIdx.y, h = blockIdx.x % c.Hkv;
   const KvqRun run = kvq_run(r.start, r.count, r.T, b);
@@ -203,7 +228,8 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_read_kernel(KvqView c, 
   if (base >= end || base + kPage <= beg) return;
   const uint8_t* unit = kvq_unit_of(c, b, page, h);
   if (unit) {
-    for (int i = threadIdx.x; i < WORDS / 4; i += NT) *((u32x4*)lds + i) = *((const u32x4*)unit + i);
+    for (int i = threadIdx.x; i < WORDS / 4; i += NT)
+      *(u32x4*)&lds[4 * i < CODES ? banked(4 * i) : 4 * i] = *((const u32x4*)unit + i);
   }
   __syncthreads();
 #pragma unroll
@@ -216,7 +242,7 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_read_kernel(KvqView c, 
       unsigned o[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        o[t] = lds[(isv ? kvq_value_at(HD, slot, d + t) : kvq_key_at(slot + t, d)) / 4];
+        o[t] = lds[banked((isv ? kvq_value_at(HD, slot, d + t) : kvq_key_at(slot + t, d)) / 4)];
         s[t] = __uint_as_float(lds[(isv ? kvq_value_scale_at(HD, slot + t) : kvq_key_scale_at(HD, slot + t)) / 4]);
       }
       if (isv) transpose4(o, w);
@@ -241,7 +267,10 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_read_kernel(KvqView c, 
   }
 }
 
-// One wave per (layer, KV head, prompt).  Entry i of the path moves from
+// Moves of single tokens: their bytes lie in 16 lines of the keys and all 32
+// of the values, as the attention's order has it, so the lines and not the
+// bytes bound it (16 prompts x 8 tokens x 256 units of hd = 128: 17 MB of
+// tokens, 17 us).  One wave per (layer, KV head, prompt).  Entry i of the path moves from
 // slot L + path[i] to L + i.  Eight entries at a time are read before any of
 // them is written; with path ascending, path[i] >= i, so that no later
 // entry's source has been written by then.
@@ -249,8 +278,6 @@ template <int HD>
 __global__ __launch_bounds__(64) void kvq_keep_kernel(KvqView c, long long layer_bytes, const int* lens,
                                                       const int* path, const int* n_path, int n, int* new_lens) {
   constexpr int CH = 8;
-  constexpr int KPL = (HD / 8 * CH + 63) / 64;   // 8-byte key pieces per lane
-  constexpr int VPL = (HD * CH + 63) / 64;       // value bytes per lane
   const int b = blockIdx.y, h = blockIdx.x % c.Hkv, layer = blockIdx.x / c.Hkv;
   const int lane = threadIdx.x;
   c.pool += layer * layer_bytes;
