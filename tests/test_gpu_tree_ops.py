@@ -234,6 +234,31 @@ def test_split_keys(kind, B, n, H, heads, hd, L):
         _check(out, q, k, v, lens, parents, [n] * B, hd ** -0.5, f"bound {bound} {kind}")
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("hd,n,causal", [(128, 64, False), (64, 61, True), (32, 64, False)])
+def test_batches_that_fill_the_chip(fmt, kind, hd, n, causal):
+    """Enough rows for waves of two row tiles (the last tiles part empty at 61 nodes), prompts of unlike lengths and node
+    counts in no order."""
+    from paper_2412_10418_amd import binding as bd
+    rng = np.random.default_rng([hd, n])
+    B, H, heads = 97, 16, 8
+    lens = rng.integers(0, 140, B).tolist()
+    lens[5], lens[90] = 0, 150
+    nodes = rng.integers(1, n + 1, B)
+    nodes[[5, 50, 90]] = n
+    cache, k, v = _filled(rng, B, lens, n, heads, hd, fmt)
+    q = (1.5 * _rows(rng, (B, n, H, hd), "f32")).to(KIND[kind])
+    parents = None if causal else np.stack([random_tree(rng, n, 3) for _ in range(B)])
+    out = bd.cdsl_op_tree_attention(cache, q, _ints(lens), None if causal else _ints(parents), n_nodes=_ints(nodes),
+                                    max_len=max(lens))
+    some = [0, 5, 17, 50, 90, 96]
+    _check(out[some], q[some], k[some], v[some], [lens[b] for b in some], None if causal else parents[some],
+           nodes[some].tolist(), hd ** -0.5, f"{fmt} {kind}")
+    for b in range(B):
+        assert torch.isfinite(out[b, :nodes[b]]).all() and not out[b, nodes[b]:].any()
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("L", [3, 2500])
 def test_nodes_that_a_prompt_lacks(kind, L):
@@ -414,11 +439,13 @@ def test_trees_are_verified(replace, B, n, V, width):
         print(f"near {near}: {np.mean(m):.2f} nodes a path", flush=True)
 
 
+@pytest.mark.parametrize("V", [3001, 40001])
 @pytest.mark.parametrize("replace", [True, False])
-def test_many_siblings_are_rejected(replace):
-    """A star of 40 siblings whose target mass is elsewhere: a chain of rejections, with duplicates among the tokens."""
+def test_many_siblings_are_rejected(replace, V):
+    """A star of 40 siblings whose target mass is elsewhere: a chain of rejections, with duplicates among the tokens (more
+    sums than long rows have launches for)."""
     rng = np.random.default_rng(31)
-    B, n, V = 6, 41, 3001
+    B, n = 6, 41
     z = rng.standard_normal((B, n, V))
     p, q = _soft(2 * z), _soft(-z)
     tokens = np.argsort(-q[:, 0], -1)[:, :n].astype(np.int32)
@@ -430,11 +457,12 @@ def test_many_siblings_are_rejected(replace):
     assert min(m) == 1
 
 
+@pytest.mark.parametrize("V", [70, 33001])
 @pytest.mark.parametrize("replace", [True, False])
-def test_rows_at_the_borders_of_the_walk(replace):
+def test_rows_at_the_borders_of_the_walk(replace, V):
     """Equal rows, one-hot rows, rows without mass, draws at 0 and just below 1, tokens and parents out of range."""
     rng = np.random.default_rng(32)
-    n, V = 6, 70
+    n = 6
     p = np.zeros((9, n, V), np.float32)
     q = np.zeros((9, n, V), np.float32)
     base = _soft(rng.standard_normal((n, V)))
@@ -465,12 +493,13 @@ def test_rows_at_the_borders_of_the_walk(replace):
     _verify(p, q, tokens, parents, u, v, replace)
 
 
-def test_sums_that_are_not_finite():
+@pytest.mark.parametrize("V", [300, 70000])
+def test_sums_that_are_not_finite(V):
     from paper_2412_10418_amd import binding as bd
-    for bad in (np.nan, np.inf):
-        p = np.full((1, 2, 300), 1 / 300, np.float32)
+    for bad in (np.nan, np.inf, -np.nan):
+        p = np.full((1, 2, V), 1 / V, np.float32)
         p[0, 0, 17] = bad
-        q = np.full_like(p, 1 / 300)
+        q = np.full_like(p, 1 / V)
         path, m, tok = bd.cdsl_op_tree_accept(torch.from_numpy(p).cuda(), torch.from_numpy(q).cuda(), _ints([[0, 17]]),
                                               _ints([[-1, -1]]), torch.zeros(1, 2, device="cuda"),
                                               torch.full((1,), 0.5, device="cuda"))
@@ -628,12 +657,12 @@ def test_steps_over_drafted_trees(fmt, kind):
             assert np.array_equal(_np(v[b, :lens[b]]), held[l][1][b].astype(np.float32))
 
 
-@pytest.mark.parametrize("bound", [60, 4000])
-def test_captured_steps_replay_as_they_run(bound):
+@pytest.mark.parametrize("bound,V", [(60, 300), (4000, 40000)])
+def test_captured_steps_replay_as_they_run(bound, V):
     """Two graphs of a step over one cache, replayed in turn on new inputs with eager steps of another cache between
     them: every replay gives the eager result's bits."""
     rng = np.random.default_rng(52)
-    B, n, H, heads, hd, V, layers = 2, 9, 4, 2, 64, 300, 2
+    B, n, H, heads, hd, layers = 2, 9, 4, 2, 64, 2
     a, e, other = (paged(np.random.default_rng(53), layers, B, 128 + bound, heads, hd, "int8") for _ in range(3))
     states = [_state(rng, B, n, H, heads, hd, V, layers, [40, 11], "f32", bound) for _ in range(2)]
     _step(other, states[0], layers)
