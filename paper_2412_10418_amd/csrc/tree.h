@@ -39,12 +39,13 @@ struct TreeAttnArgs {
   float* part_ml;          // [nsplit][B * n * H][2]
   int nsplit, row_groups;
   int split_pages;         // pages per key split, at least
-  int wg_tiles;            // row tiles per workgroup (tree_many_kernel)
+  int wg_tiles;            // row tiles (of 16) per workgroup
 };
 
 struct TreeAttnPlan {
-  int few;                 // 1, 2: tree_few_kernel with so many row tiles; 0: tree_many_kernel
-  int rpw, wg_tiles;       // its row tiles per wave and per workgroup
+  int few;                 // 1, 2: tree_few_kernel with so many row tiles
+  bool wide;               // tree_wide_kernel; else tree_many_kernel
+  int wg_tiles;            // row tiles (of 16) per workgroup
   int row_groups, nsplit, split_pages;
   size_t workspace;
 };

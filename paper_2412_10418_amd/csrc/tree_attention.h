@@ -22,11 +22,12 @@
 // result rounds by as much) for bf16.  Two planes would lose 2^-16 of each
 // probability: 2.5e-6 of the result, where fp32 products give 0.8e-6.
 //
-// Two kernels.  Few rows (one or two tiles): the codes go from memory
+// Three kernels.  Few rows (one or two tiles): the codes go from memory
 // straight to the registers of the wave that uses them, and the waves of a
 // workgroup take different pages (tree_few_kernel).  More rows: the
 // workgroup's waves take different rows, and the pages are converted once for
-// all of them through LDS (tree_many_kernel).
+// all of them through LDS (tree_many_kernel; tree_wide_kernel with tiles of 32
+// rows where they fill the chip).
 #pragma once
 #include <type_traits>
 
@@ -38,6 +39,7 @@ namespace {
 
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 
 constexpr float kLazy = 8.f;   // log2 units that the running maximum may lag behind
 
@@ -183,12 +185,85 @@ __device__ __forceinline__ void tree_masks(const TreeAttnArgs& a, const TreeSpan
   __syncthreads();
 }
 
+// Eight entries of q.
+template <typename QT>
+__device__ __forceinline__ void load_q8(const QT* p, float (&x)[8]) {
+  if constexpr (sizeof(QT) == 2) {
+    const bf16x8 v = *(const bf16x8*)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+  } else {
+    const f32x4 v0 = *(const f32x4*)p, v1 = *(const f32x4*)(p + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = e < 4 ? v0[e & 3] : v1[e & 3];
+  }
+}
+
+// The power of two that brings a row of q to a largest entry in [1, 2), from
+// the largest bit pattern of |q|: what the entries are multiplied by (with the
+// sign of the softmax scale; 0 for a scale of 0), and what a score of the
+// result counts in log2 units.  Rows of zeros and of the smallest numbers
+// count as 2^-126; a NaN or an infinity stays one (its scores are NaN).
+struct QScale {
+  float down, rm;
+};
+__device__ __forceinline__ QScale q_scale(float scale_log2, unsigned top) {
+  const int e = max((int)(top >> 23), 1) - 127;
+  // (2^-127 and 2^-128 are subnormal, which products keep)
+  return {__builtin_ldexpf(scale_log2 < 0.f ? -1.f : scale_log2 > 0.f ? 1.f : 0.f, -e),
+          scale_log2 == 0.f ? 1.f : __builtin_ldexpf(fabsf(scale_log2), e)};
+}
+template <int QP>
+__device__ __forceinline__ void q_planes(const float (&x)[8], float down, f16x8 (&q)[QP]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float y = x[k] * down;
+    const _Float16 hi = (_Float16)y;
+    q[0][k] = hi;
+    if constexpr (QP > 1) q[1][k] = (_Float16)(y - (float)hi);
+  }
+}
+
+// Probabilities times s_v as bf16 planes: one, rounded; or three by
+// truncation, 8 bits each, where each rest is exact.
+template <int PP>
+__device__ __forceinline__ void p_planes(float (&w)[8], bf16x8 (&pf)[PP]) {
+  if constexpr (PP == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pf[0][e] = (bf16)w[e];
+  } else {
+    union {
+      unsigned u[4];
+      bf16x8 v;
+    } o;
+#pragma unroll
+    for (int pl = 0; pl < PP; ++pl) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        o.u[e] = __builtin_amdgcn_perm(__float_as_uint(w[2 * e + 1]), __float_as_uint(w[2 * e]), 0x07060302);
+      pf[pl] = o.v;
+      if (pl + 1 < PP)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] -= __uint_as_float(__float_as_uint(w[e]) & 0xffff0000u);
+    }
+  }
+}
+
+template <typename QT>
+__device__ __forceinline__ void store4(QT* o, f32x4 y) {
+  if constexpr (sizeof(QT) == 4) *(f32x4*)o = y;
+  else *(bf16x4*)o = (bf16x4){(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+}
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float halves_max(float v) {   // xor 32
+  const u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
+}
 // Over the four lanes of a row (xor 16 and 32).
 __device__ __forceinline__ float groups_max(float v) {
-  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-  u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
-  t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = halves_max(v);
+  const u32x2 t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
 }
 
@@ -215,35 +290,16 @@ struct RowTile {
     unsigned top = 0;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      if constexpr (sizeof(QT) == 2) {
-        const bf16x8 v = *(const bf16x8*)(qp + 32 * s);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] = (float)v[e];
-      } else {
-        const f32x4 v0 = *(const f32x4*)(qp + 32 * s), v1 = *(const f32x4*)(qp + 32 * s + 4);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] = e < 4 ? v0[e & 3] : v1[e & 3];
-      }
+      load_q8<QT>(qp + 32 * s, x[s]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[s][e]) & 0x7fffffffu);
     }
     top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
     top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
-    // 2^e <= max|q| < 2^(e+1); rows of zeros and the smallest numbers as 2^-126,
-    // a NaN or an infinity stays one (its scores are NaN)
-    const int e = max((int)(top >> 23), 1) - 127;
-    const float down = __builtin_ldexpf(a.scale_log2 < 0.f ? -1.f : a.scale_log2 > 0.f ? 1.f : 0.f, -e);
-    rm = a.scale_log2 == 0.f ? 1.f : __builtin_ldexpf(fabsf(a.scale_log2), e);
+    const QScale qs = q_scale(a.scale_log2, top);
+    rm = qs.rm;
 #pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        // (2^-127 and 2^-128 are subnormal, which products keep)
-        const float y = x[s][k] * down;
-        const _Float16 hi = (_Float16)y;
-        q[s][0][k] = hi;
-        if constexpr (QP > 1) q[s][1][k] = (_Float16)(y - (float)hi);
-      }
+    for (int s = 0; s < S; ++s) q_planes<QP>(x[s], qs.down, q[s]);
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
     m = -INFINITY;
@@ -285,26 +341,7 @@ struct RowTile {
       l += p;
       w[e] = p * vs[e];
     }
-    if constexpr (PP == 1) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pf[0][e] = (bf16)w[e];
-    } else {
-      // planes by truncation: 8 bits each, and each rest is exact
-      union {
-        unsigned u[4];
-        bf16x8 v;
-      } o;
-#pragma unroll
-      for (int pl = 0; pl < PP; ++pl) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          o.u[e] = __builtin_amdgcn_perm(__float_as_uint(w[2 * e + 1]), __float_as_uint(w[2 * e]), 0x07060302);
-        pf[pl] = o.v;
-        if (pl + 1 < PP)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] -= __uint_as_float(__float_as_uint(w[e]) & 0xffff0000u);
-      }
-    }
+    p_planes<PP>(w, pf);
   }
 
   __device__ __forceinline__ void finish() {
@@ -321,9 +358,7 @@ struct RowTile {
       QT* o = (QT*)a.out + row * HD + 4 * lg;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const f32x4 y = acc[d] * inv;
-        if constexpr (sizeof(QT) == 4) *(f32x4*)(o + 16 * d) = y;
-        else *(bf16x4*)(o + 16 * d) = (bf16x4){(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+        store4<QT>(o + 16 * d, acc[d] * inv);
       }
     } else {
       const long long prow = (long long)t.split * a.c.B * a.n * a.H + row;
@@ -551,19 +586,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
 }
 
 // Workgroup = (key split, prompt x KV head, group of a.wg_tiles row tiles);
-// wave w takes tiles w RPW .. .  A page is converted once for all waves: its
+// wave w takes tile w.  A page is converted once for all waves: its
 // codes come in as 16 bytes a thread, two pages before they are needed, and go
 // to LDS as f16 (keys) and bf16 (values) in operand order.
-template <int HD, int FMT, typename QT, int RPW>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RPW == 1 ? 3 : 2))) void tree_many_kernel(
-    TreeAttnArgs a) {
+template <int HD, int FMT, typename QT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void tree_many_kernel(TreeAttnArgs a) {
   using Row = RowTile<HD, QT>;
   constexpr int NT = 256, W = 4;
   constexpr int S = Row::S, DT = Row::DT;
   constexpr int UNIT = kvq_unit_bytes(HD);
   constexpr int CH = 2 * S * 64;                     // 16-byte chunks of codes in a unit
   constexpr int PER = (CH + NT - 1) / NT;
-  constexpr int ROWS = 16 * W * RPW;
+  constexpr int ROWS = 16 * W;
   __shared__ __attribute__((aligned(16))) u32x4 tile[2][2 * CH];   // [keys: S][half] [values: DT], 64 lanes each
   __shared__ __attribute__((aligned(16))) float scale[2][2 * kPage];
   __shared__ uint32_t masks[ROWS * kTreeWords];
@@ -574,7 +608,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RPW == 1 ? 
   const TreeSpan t = tree_span(a, a.wg_tiles);
   if (t.none) return;   // uniform over the workgroup
   const int npages = t.end - t.beg;
-  const int wrow = t.row0 + 16 * RPW * wave;
+  const int wrow = t.row0 + 16 * wave;
   const int wend = min(t.row0 + 16 * a.wg_tiles, t.nrows);
   const bool has_rows = wrow < wend;
 
@@ -629,14 +663,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RPW == 1 ? 
     load(0, 0);
     load(1, 1);
   }
-  Row row[RPW];
-#pragma unroll
-  for (int r = 0; r < RPW; ++r) {
-    row[r].init(a, t, wrow + 16 * r + lr, lg);
-    row[r].valid = wrow + 16 * r + lr < wend;
-  }
+  Row row[1];
+  row[0].init(a, t, wrow + lr, lg);
+  row[0].valid = wrow + lr < wend;
   // the last node of the wave's rows: later pages hold nothing for it
-  const int wlast = (min(wrow + 16 * RPW, wend) - 1) / a.G;
+  const int wlast = (min(wrow + 16, wend) - 1) / a.G;
   const bool tree = a.parents != nullptr && a.n > 1;
   if (tree) tree_masks(a, t, masks, par, NT);
   if (npages > 0) put(0, 0);
@@ -647,16 +678,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RPW == 1 ? 
     const int page = t.beg + it;
     load(it + 2, buf);
     if (has_rows && !(MASKED && page * kPage > t.L + wlast)) {
-      f32x4 sc[RPW][2];
-#pragma unroll
-      for (int r = 0; r < RPW; ++r) sc[r][0] = sc[r][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      f32x4 sc[1][2] = {{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}};
 #pragma unroll
       for (int s = 0; s < S; ++s)
         score_step(row, s, *(const f16x8*)&tile[buf][(2 * s) * 64 + lane],
                    *(const f16x8*)&tile[buf][(2 * s + 1) * 64 + lane], sc);
       const f32x4 ks[2] = {*(const f32x4*)&scale[buf][4 * lg], *(const f32x4*)&scale[buf][16 + 4 * lg]};
       const f32x4 vs[2] = {*(const f32x4*)&scale[buf][kPage + 4 * lg], *(const f32x4*)&scale[buf][kPage + 16 + 4 * lg]};
-      bf16x8 pf[RPW][Row::PP];
+      bf16x8 pf[1][Row::PP];
       page_softmax<MASKED>(row, sc, ks, vs, tree, page * kPage - t.L, t.node0, masks, lg, pf);
 #pragma unroll
       for (int d = 0; d < DT; d += 2)
@@ -679,10 +708,254 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RPW == 1 ? 
     if (it + 1 < npages) step(std::true_type{}, it + 1, 1);
   }
   if (!has_rows) return;
+  row[0].finish();
+  row[0].store(a, t, lg);
+}
+
+// A tile of 32 rows in a wave: lane (row lane % 32, half h = lane / 32).
+template <int HD, typename QT>
+struct WideTile {
+  static constexpr int S = HD / 16, DT = HD / 32;
+  static constexpr int QP = sizeof(QT) == 4 ? 2 : 1, PP = sizeof(QT) == 4 ? 3 : 1;
+  f16x8 q[S][QP];        // dims 16 s + 8 h .. +7
+  float rm;
+  f32x16 acc[DT];        // dims 32 d + 8 (i / 4) + 4 h + i % 4
+  float m, l;
+  int node, head;
+  bool valid;
+};
+
+// tree_many_kernel with tiles of 32 rows (MFMA 32x32x16): half the matrix
+// instructions and LDS reads.  A matrix instruction keeps the SIMD from
+// issuing vector ones for about eight cycles whatever its size (a wave of
+// either beside a wave of vector work: 376 us for 16x16x32, 326 for 32x32x16,
+// where each alone takes 250), and the vector work of the softmax is as long
+// as the products.  Executed products: 0.96 PFLOP/s in fp32 (40 instructions a
+// tile and page; 64 prompts x 8 KV heads of 16 tiles at 1024 tokens), 1.19 (8 x
+// 8 of 128 tiles, causal), where a product of 8192^3 reaches 1.40.  Scores: lane (row, h) holds slots 8 j + 4 h + e, j < 4, e < 4,
+// which in that order are its operand of the two value products of 16 slots.
+template <int HD, int FMT, typename QT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void tree_wide_kernel(TreeAttnArgs a) {
+  using Row = WideTile<HD, QT>;
+  constexpr int NT = 256, W = 4;
+  constexpr int S = Row::S, DT = Row::DT, QP = Row::QP, PP = Row::PP;
+  constexpr int UNIT = kvq_unit_bytes(HD);
+  constexpr int CH = 4 * HD;                         // 16-byte chunks of codes in a unit
+  constexpr int PER = (CH + NT - 1) / NT;
+  constexpr int ROWS = 32 * W;
+  // operands of 64 lanes: keys [S], values [DT][2]
+  __shared__ __attribute__((aligned(16))) u32x4 ktile[2][S * 64], vtile[2][DT * 2 * 64];
+  __shared__ __attribute__((aligned(16))) float scale[2][2 * kPage];
+  __shared__ uint32_t masks[ROWS * kTreeWords];
+  __shared__ int par[kTreeMax];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, h = lane >> 5;
+  const TreeSpan t = tree_span(a, a.wg_tiles);
+  if (t.none) return;   // uniform over the workgroup
+  const int npages = t.end - t.beg;
+  const int wrow = t.row0 + 32 * wave;
+  const int wend = min(t.row0 + 16 * a.wg_tiles, t.nrows);
+  const bool has_rows = wrow < wend;
+
+  const int* table = a.c.table + (long long)t.b * a.c.table_stride + t.beg;
+  // Two pages in flight, as in tree_many_kernel.
+  u32x4 raw[2][PER];
+  float sraw[2];
+  bool bad[2] = {false, false};
+  int id_next = npages > 0 ? table[0] : 0;
+  auto load = [&](int it, int slot) __attribute__((always_inline)) {
+    const int id = id_next;
+    id_next = table[min(it + 1, npages - 1)];
+    bad[slot] = id < 0 || id >= a.c.pages;
+    const uint8_t* u = a.c.pool + ((long long)(bad[slot] ? 0 : id) * a.c.Hkv + t.kvh) * UNIT;
 #pragma unroll
-  for (int r = 0; r < RPW; ++r) {
-    row[r].finish();
-    row[r].store(a, t, lg);
+    for (int c = 0; c < PER; ++c)
+      if (CH % NT == 0 || tid + NT * c < CH) raw[slot][c] = *((const u32x4*)u + tid + NT * c);
+    sraw[slot] = *((const float*)(u + 2 * kPage * HD) + lane);
+  };
+  auto put = [&](int it, int buf) __attribute__((always_inline)) {
+    const int page = t.beg + it;
+#pragma unroll
+    for (int c = 0; c < PER; ++c) {
+      const int i = tid + NT * c;
+      if (CH % NT != 0 && i >= CH) continue;
+      // chunk (dims / 32, quarter g, x = lane % 16)
+      const int s = i >> 6, g = lane >> 4, x = lane & 15;
+      const u32x4 w = raw[buf][c];
+      if (CH % (2 * NT) == 0 ? c < PER / 2 : s < HD / 32) {   // keys x and x + 16, dims 32 s + 8 g .. +7
+        union {
+          f16x8 h8;
+          u32x4 u;
+        } k0, k1;
+        k0.h8 = codes_f16<FMT>(w.x, w.y);
+        k1.h8 = codes_f16<FMT>(w.z, w.w);
+        u32x4* at = &ktile[buf][(2 * s + (g >> 1)) * 64 + (g & 1) * 32 + x];
+        at[0] = k0.u;
+        at[16] = k1.u;
+      } else {   // dims 32 d + x and + 16, slots 4 g .. +3 and 16 + 4 g .. +3
+        u32x4 v = w;
+        if (FMT == kE4M3 && (page + 1) * kPage > t.L) v = hold_values(v, t.L + t.nb - page * kPage, g);
+        union {
+          bf16x8 b8;
+          uint2 u[2];
+        } v0, v1;
+        v0.b8 = codes_bf16<FMT>(v.x, v.y);
+        v1.b8 = codes_bf16<FMT>(v.z, v.w);
+        const int d = s - HD / 32;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint2* at = (uint2*)&vtile[buf][(2 * d + k) * 64 + (g & 1) * 32 + x] + (g >> 1);
+          at[0] = v0.u[k];
+          at[32] = v1.u[k];
+        }
+      }
+    }
+    // a page that does not exist: rows that see one of its keys are NaN
+    if (wave == 0) scale[buf][lane] = bad[buf] && lane < kPage ? __uint_as_float(0x7fc00000u) : sraw[buf];
+  };
+
+  if (npages > 0) {
+    load(0, 0);
+    load(1, 1);
+  }
+  Row row;
+  {
+    const int r0 = wrow + lr;
+    row.valid = r0 < wend;
+    const int r = r0 < t.nrows ? r0 : t.nrows - 1;
+    row.node = r / a.G;
+    row.head = t.kvh * a.G + r % a.G;
+    const QT* qp = (const QT*)a.q + t.b * a.qsb + row.node * a.qst + (long long)row.head * HD + 8 * h;
+    float x[S][8];
+    unsigned top = 0;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      load_q8<QT>(qp + 16 * s, x[s]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[s][e]) & 0x7fffffffu);
+    }
+    top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
+    const QScale qs = q_scale(a.scale_log2, top);
+    row.rm = qs.rm;
+#pragma unroll
+    for (int s = 0; s < S; ++s) q_planes<QP>(x[s], qs.down, row.q[s]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) row.acc[d][i] = 0.f;
+    row.m = -INFINITY;
+    row.l = t.over ? __uint_as_float(0x7fc00000u) : 0.f;
+  }
+  // the last node of the wave's rows: later pages hold nothing for it
+  const int wlast = (min(wrow + 32, wend) - 1) / a.G;
+  const bool tree = a.parents != nullptr && a.n > 1;
+  if (tree) tree_masks(a, t, masks, par, NT);
+  if (npages > 0) put(0, 0);
+  __syncthreads();
+
+  auto step = [&](auto masked, int it, int buf) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const int page = t.beg + it;
+    load(it + 2, buf);
+    if (has_rows && !(MASKED && page * kPage > t.L + wlast)) {
+      f32x16 sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const f16x8 k = *(const f16x8*)&ktile[buf][s * 64 + lane];
+#pragma unroll
+        for (int pl = 0; pl < QP; ++pl)
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, row.q[s][pl], sc, 0, 0, 0);
+      }
+      float p[16], v[16];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 ks = *(const f32x4*)&scale[buf][8 * j + 4 * h], vs = *(const f32x4*)&scale[buf][kPage + 8 * j + 4 * h];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[4 * j + e] = sc[4 * j + e] * ks[e];
+          v[4 * j + e] = vs[e];
+        }
+      }
+      if constexpr (MASKED) {
+        const int i0 = page * kPage - t.L;
+        const unsigned vis = (tree ? slots_of_tree(i0, masks + (row.node - t.node0) * kTreeWords)
+                                   : slots_of_chain(i0, row.node)) >> (4 * h);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool seen = vis >> (8 * (i / 4) + i % 4) & 1u;
+          p[i] = seen ? p[i] : -INFINITY;
+          v[i] = seen ? v[i] : 0.f;   // the scale of a hidden slot may be anything
+        }
+      }
+      float mt = p[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mt = fmaxf(mt, p[i]);
+      mt = halves_max(mt) * row.rm;
+      const bool raise = mt > row.m + kLazy;
+      if (__ballot(raise)) {
+        const float to = raise ? mt : row.m;
+        const float corr = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(row.m - to);
+        row.l *= corr;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) row.acc[d] *= corr;
+        row.m = to;
+      }
+      const float mu = row.m == -INFINITY ? 0.f : row.m;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        bf16x8 pf[PP];
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(p[8 * k + e], row.rm, -mu));
+          row.l += x;
+          w[e] = x * v[8 * k + e];
+        }
+        p_planes<PP>(w, pf);
+        bf16x8 vf[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) vf[d] = *(const bf16x8*)&vtile[buf][(2 * d + k) * 64 + lane];
+#pragma unroll
+        for (int pl = 0; pl < PP; ++pl)
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+            row.acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d], pf[pl], row.acc[d], 0, 0, 0);
+      }
+    }
+    put(it + 1, buf ^ 1);
+    __syncthreads();
+  };
+  const int plain = min(npages, max(0, t.L / kPage - t.beg)) & ~1;
+  int it = 0;
+  for (; it < plain; it += 2) {
+    step(std::false_type{}, it, 0);
+    step(std::false_type{}, it + 1, 1);
+  }
+  for (; it < npages; it += 2) {
+    step(std::true_type{}, it, 0);
+    if (it + 1 < npages) step(std::true_type{}, it + 1, 1);
+  }
+  if (!has_rows) return;
+  row.l += __shfl_xor(row.l, 32, 64);
+  if (!row.valid) return;
+  const long long out = ((long long)t.b * a.n + row.node) * a.H + row.head;
+  const float inv = 1.f / row.l;
+  const long long prow = (long long)t.split * a.c.B * a.n * a.H + out;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 y = {row.acc[d][4 * j], row.acc[d][4 * j + 1], row.acc[d][4 * j + 2], row.acc[d][4 * j + 3]};
+      const int at = 32 * d + 8 * j + 4 * h;
+      if (a.nsplit == 1) store4<QT>((QT*)a.out + out * HD + at, y * inv);
+      else *(f32x4*)(a.part_o + prow * HD + at) = y;
+    }
+  if (a.nsplit > 1 && h == 0) {
+    a.part_ml[prow * 2] = row.m;
+    a.part_ml[prow * 2 + 1] = row.l;
   }
 }
 
@@ -739,8 +1012,8 @@ hipError_t tree_attn_rows(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStrea
   const unsigned grid = (unsigned)((long long)p.row_groups * p.nsplit * a.c.B * a.c.Hkv);
   if (p.few == 1) tree_few_kernel<HD, FMT, QT, 1><<<grid, 256, 0, st>>>(a);
   else if (p.few == 2) tree_few_kernel<HD, FMT, QT, 2><<<grid, 256, 0, st>>>(a);
-  else if (p.rpw == 1) tree_many_kernel<HD, FMT, QT, 1><<<grid, 256, 0, st>>>(a);
-  else tree_many_kernel<HD, FMT, QT, 2><<<grid, 256, 0, st>>>(a);
+  else if (!p.wide) tree_many_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
+  else tree_wide_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const long long rows = (long long)a.c.B * a.n * a.H;

@@ -14,16 +14,15 @@ TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len) {
   TreeAttnPlan p{};
   const int tiles = (int)(((long long)n * (H / Hkv) + 15) / 16);
   p.few = tiles <= 2 ? tiles : 0;
-  // Two row tiles a wave read every fragment of a page once for both, and take
-  // 0.93 of the time a tile where they fill the chip (64 prompts x 8 KV heads
-  // of 16 tiles at 1024 tokens: 181 against 190 us in fp32, 116 against 130 in
-  // bf16); not where they leave slots empty (17 tiles: 237 against 218) or
-  // give less than three workgroups a CU (16 pairs of 128 tiles: 105 against
-  // 87).
+  // Tiles of 32 rows take 0.95 (fp32) or 0.85 (bf16) of the time where they
+  // fill the chip (64 prompts x 8 KV heads of 16 tiles of 16 at 1024 tokens: 190
+  // against 202 us, 120 against 138), not where they leave slots empty (17
+  // tiles: 231 against 228) or give less than three workgroups a CU (16 pairs of
+  // 128 tiles: 97 against 82).
   const long long pairs = (long long)B * Hkv;
   const long long one = (tiles + 3) / 4, two = (tiles + 7) / 8;
-  p.rpw = !p.few && pairs * two >= 768 && 8 * two * 0.93 < 4 * one ? 2 : 1;
-  const int most_tiles = p.few ? p.few : 4 * p.rpw;
+  p.wide = !p.few && pairs * two >= 768 && 8 * two * 0.93 < 4 * one;
+  const int most_tiles = p.few ? p.few : p.wide ? 8 : 4;
   p.row_groups = (tiles + most_tiles - 1) / most_tiles;
   p.wg_tiles = (tiles + p.row_groups - 1) / p.row_groups;
   // Keys are split until there are two workgroups a CU; a split has eight pages
