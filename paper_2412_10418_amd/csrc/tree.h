@@ -24,6 +24,7 @@ hipError_t kvq_keep_launch(const KvqView& c, int n_layers, long long layer_bytes
                            const int* n_path, int n, int* new_lens, hipStream_t st);
 
 constexpr int kTreeMaxSplits = 64;
+constexpr int kTreeShared = 64;   // prompts that share the key splits by their lengths
 
 struct TreeAttnArgs {
   KvqView c;
@@ -35,9 +36,9 @@ struct TreeAttnArgs {
   const int* parents;      // null: causal
   int n, H, G;
   float scale_log2;        // softmax scale * log2(e)
-  float* part_o;           // [nsplit][B * n * H][hd]
-  float* part_ml;          // [nsplit][B * n * H][2]
-  int nsplit, row_groups;
+  float* part_o;           // [B nsplit][n * H][hd]
+  float* part_ml;          // [B nsplit][n * H][2]
+  int nsplit, row_groups;  // key splits of a prompt, of all prompts / B
   int split_pages;         // pages per key split, at least
   int wg_tiles;            // row tiles (of 16) per workgroup
 };

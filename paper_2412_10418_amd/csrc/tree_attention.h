@@ -111,10 +111,61 @@ __device__ __forceinline__ u32x4 hold_values(u32x4 w, int held, int lg) {
   return (u32x4){w.x & mA, w.y & mB, w.z & mA, w.w & mB};
 }
 
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float halves_max(float v) {   // xor 32
+  const u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
+}
+// Over the four lanes of a row (xor 16 and 32).
+__device__ __forceinline__ float groups_max(float v) {
+  v = halves_max(v);
+  const u32x2 t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
+}
+// Over a wave, by lane moves.
+__device__ __forceinline__ float lanes_sum(float v) {
+  const u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(t.x) + __uint_as_float(t.y);
+  const u32x2 u = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(u.x) + __uint_as_float(u.y);
+  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xF, 0xF, true));   // rotations of 16
+  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x124, 0xF, 0xF, true));
+  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x122, 0xF, 0xF, true));
+  return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x121, 0xF, 0xF, true));
+}
+
+// Key splits of a batch of 2 to 64 prompts.  The launch has room for B nsplit of
+// them; a prompt takes a share in proportion to its pages (its "parts", one at
+// least, of a.split_pages pages or more), so that a long prompt among short
+// ones does not hold up the rest (8 prompts of up to 32768 tokens: 75 -> 69 us;
+// one of 16384 among 31 of 512: 60 -> 24).  Lane j of a wave finds the parts of prompt
+// j.  ceil(w x) parts of weights w come to at most x sum(w) + B, so the last
+// of the four x fits; the first that does is taken.  (Weights up to 2^25 and
+// 1e-5 under the bound: far more than the rounding of these sums.)
+__device__ __forceinline__ int tree_parts(const TreeAttnArgs& a, int lane) {
+  const int B = a.c.B;
+  float w = 0.f;
+  if (lane < B) {
+    const int L = max(a.lens[lane], 0), nb = a.n_nodes ? min(max(a.n_nodes[lane], 0), a.n) : a.n;
+    const long long toks = (long long)L + nb;
+    if (toks <= (long long)a.c.table_stride * kPage) w = (float)min((toks + kPage - 1) / kPage, 1ll << 25);
+  }
+  const float room = (float)(B * a.nsplit), per = 0.99999f / fmaxf(lanes_sum(w), 1.f);
+  const float most = 1.f / (float)a.split_pages;
+  float k[4], sum[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float x = fminf((room - (float)(B * i) / 3.f) * per, most);
+    k[i] = lane < B ? fminf(fmaxf(ceilf(w * x), 1.f), (float)kTreeMaxSplits) : 0.f;
+    sum[i] = lanes_sum(k[i]);
+  }
+  return (int)(sum[0] <= room ? k[0] : sum[1] <= room ? k[1] : sum[2] <= room ? k[2] : k[3]);
+}
+
 // The prompt, KV head, keys and rows of a workgroup that takes `tiles` row
 // tiles of a (prompt, KV head).
 struct TreeSpan {
-  int b, kvh, split, nrows, row0, L, nb, node0, node1, beg, end;
+  int b, kvh, slot, parts, nrows, row0, L, nb, node0, node1, beg, end;
   bool over, none;
 };
 
@@ -133,36 +184,51 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs& a, int tiles) 
     chunk = full + x / NR;
     rg = x % NR;
   }
-  t.split = chunk % a.nsplit;
-  const int pair = chunk / a.nsplit;
-  t.b = pair / a.c.Hkv;
-  t.kvh = pair % a.c.Hkv;
-  // Prompts of unlike lengths: the longest first, so that the last workgroups
-  // to start are short (one lane a prompt finds its place).
-  if (a.nsplit == 1 && a.c.B > 1 && a.c.B <= 64) {
-    const int lane = threadIdx.x & 63;
-    const int len = lane < a.c.B ? a.lens[lane] : 0;
+  const int lane = threadIdx.x & 63, B = a.c.B;
+  t.slot = chunk / a.c.Hkv;
+  t.kvh = chunk % a.c.Hkv;
+  t.b = t.slot / a.nsplit;
+  t.parts = a.nsplit;
+  int part = t.slot % a.nsplit;
+  bool spare = false;
+  if (B > 1 && B <= kTreeShared && a.nsplit > 1) {
+    const int k = tree_parts(a, lane);
+    int base = 0;
+    spare = true;
+    for (int j = 0; j < B; ++j) {
+      const int kj = __builtin_amdgcn_readlane(k, j);
+      if (spare && t.slot < base + kj) {
+        t.b = j;
+        t.parts = kj;
+        part = t.slot - base;
+        spare = false;
+      }
+      base += kj;
+    }
+  } else if (B > 1 && B <= kTreeShared) {
+    // Prompts of unlike lengths: the longest first, so that the last workgroups
+    // to start are short (one lane a prompt finds its place).
+    const int len = lane < B ? a.lens[lane] : 0;
     int place = 0;
-    for (int j = 0; j < a.c.B; ++j) {
+    for (int j = 0; j < B; ++j) {
       const int l = __builtin_amdgcn_readlane(len, j);
       place += l > len || (l == len && j < lane) ? 1 : 0;
     }
-    t.b = __builtin_ctzll(__ballot(lane < a.c.B && place == t.b));
+    t.b = __builtin_ctzll(__ballot(lane < B && place == t.b));
   }
   t.nb = a.n_nodes ? min(max(a.n_nodes[t.b], 0), a.n) : a.n;
   t.nrows = t.nb * a.G;
   t.row0 = rg * 16 * tiles;
-  t.none = t.row0 >= t.nrows;
+  t.none = spare || t.row0 >= t.nrows;
   t.L = max(a.lens[t.b], 0);
   t.node0 = t.row0 / a.G;
   t.node1 = (min(t.row0 + 16 * tiles, t.nrows) - 1) / a.G;
   // a prompt that its table cannot hold has no answer: NaN, and no page read
   t.over = (long long)t.L + t.nb > (long long)a.c.table_stride * kPage;
-  const int pages = t.over ? 0 : (t.L + t.nb + kPage - 1) / kPage;
-  // splits of one size whatever the prompt's length: those past its end are empty
-  const int per = max(a.split_pages, (pages + a.nsplit - 1) / a.nsplit);
-  t.beg = (int)min((long long)t.split * per, (long long)pages);
-  t.end = t.over ? 0 : (int)min(min((long long)t.beg + per, (long long)pages), (long long)((t.L + t.node1) / kPage + 1));
+  const int pages = t.over ? 0 : (int)(((long long)t.L + t.nb + kPage - 1) / kPage);
+  const int per = (pages + t.parts - 1) / t.parts;
+  t.beg = (int)min((long long)part * per, (long long)pages);
+  t.end = t.over ? 0 : (int)min(min((long long)t.beg + per, (long long)pages), ((long long)t.L + t.node1) / kPage + 1);
   return t;
 }
 
@@ -255,18 +321,6 @@ __device__ __forceinline__ void store4(QT* o, f32x4 y) {
   else *(bf16x4*)o = (bf16x4){(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
 }
 
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ float halves_max(float v) {   // xor 32
-  const u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
-}
-// Over the four lanes of a row (xor 16 and 32).
-__device__ __forceinline__ float groups_max(float v) {
-  v = halves_max(v);
-  const u32x2 t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(t.x), __uint_as_float(t.y));
-}
-
 // One tile of 16 rows in a wave: lane (row lr = lane % 16, group lg = lane / 16).
 template <int HD, typename QT>
 struct RowTile {
@@ -353,7 +407,7 @@ struct RowTile {
   __device__ __forceinline__ void store(const TreeAttnArgs& a, const TreeSpan& t, int lg) {
     if (!valid) return;
     const long long row = ((long long)t.b * a.n + node) * a.H + head;
-    if (a.nsplit == 1) {
+    if (t.parts == 1) {
       const float inv = 1.f / l;
       QT* o = (QT*)a.out + row * HD + 4 * lg;
 #pragma unroll
@@ -361,7 +415,7 @@ struct RowTile {
         store4<QT>(o + 16 * d, acc[d] * inv);
       }
     } else {
-      const long long prow = (long long)t.split * a.c.B * a.n * a.H + row;
+      const long long prow = ((long long)t.slot * a.n + node) * a.H + head;
       float* po = a.part_o + prow * HD + 4 * lg;
 #pragma unroll
       for (int d = 0; d < DT; ++d) *(f32x4*)(po + 16 * d) = acc[d];
@@ -943,17 +997,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
   if (!row.valid) return;
   const long long out = ((long long)t.b * a.n + row.node) * a.H + row.head;
   const float inv = 1.f / row.l;
-  const long long prow = (long long)t.split * a.c.B * a.n * a.H + out;
+  const long long prow = ((long long)t.slot * a.n + row.node) * a.H + row.head;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const f32x4 y = {row.acc[d][4 * j], row.acc[d][4 * j + 1], row.acc[d][4 * j + 2], row.acc[d][4 * j + 3]};
       const int at = 32 * d + 8 * j + 4 * h;
-      if (a.nsplit == 1) store4<QT>((QT*)a.out + out * HD + at, y * inv);
+      if (t.parts == 1) store4<QT>((QT*)a.out + out * HD + at, y * inv);
       else *(f32x4*)(a.part_o + prow * HD + at) = y;
     }
-  if (a.nsplit > 1 && h == 0) {
+  if (t.parts > 1 && h == 0) {
     a.part_ml[prow * 2] = row.m;
     a.part_ml[prow * 2 + 1] = row.l;
   }
@@ -966,16 +1020,22 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeAttnArgs a) {
   const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= rows) return;
-  if (a.n_nodes) {
-    const int nd = (int)(row / a.H % a.n), b = (int)(row / a.H / a.n);
-    if (nd >= a.n_nodes[b]) return;
+  const int per_b = a.n * a.H, b = (int)(row / per_b), at = (int)(row % per_b);
+  if (a.n_nodes && at / a.H >= a.n_nodes[b]) return;
+  // its prompt's splits (tree_span)
+  int ns = a.nsplit, slot = b * a.nsplit;
+  if (a.c.B > 1 && a.c.B <= kTreeShared) {
+    const int k = tree_parts(a, lane);
+    ns = __builtin_amdgcn_readlane(k, b);
+    if (ns == 1) return;   // written by tree_*_kernel
+    slot = (int)lanes_sum(lane < b ? (float)k : 0.f);
   }
+  const long long part = (long long)slot * per_b + at;
   constexpr int PER = (HD + 63) / 64;
-  const int ns = a.nsplit;
   float ms = -INFINITY, ls = 0.f;
   if (lane < ns) {
-    ms = a.part_ml[((long long)lane * rows + row) * 2];
-    ls = a.part_ml[((long long)lane * rows + row) * 2 + 1];
+    ms = a.part_ml[(part + (long long)lane * per_b) * 2];
+    ls = a.part_ml[(part + (long long)lane * per_b) * 2 + 1];
   }
   const float mx = wave_max(ms);
   // a split whose keys this row does not see has m = -inf, l = 0; one with a
@@ -990,7 +1050,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeAttnArgs a) {
 #pragma unroll
       for (int u = 0; u < PER; ++u) {
         const int d = lane + 64 * u;
-        o[k][u] = s0 + k < ns && d < HD ? a.part_o[((long long)(s0 + k) * rows + row) * HD + d] : 0.f;
+        o[k][u] = s0 + k < ns && d < HD ? a.part_o[(part + (long long)(s0 + k) * per_b) * HD + d] : 0.f;
       }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {

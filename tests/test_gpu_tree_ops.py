@@ -234,6 +234,43 @@ def test_split_keys(kind, B, n, H, heads, hd, L):
         _check(out, q, k, v, lens, parents, [n] * B, hd ** -0.5, f"bound {bound} {kind}")
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,H,heads,hd,L", [(2, 1, 8, 1, 32, 40000), (31, 1, 8, 2, 64, 2600), (64, 2, 8, 2, 32, 9000),
+                                              (65, 1, 2, 1, 32, 1500), (3, 70, 2, 1, 128, 3000), (9, 40, 4, 2, 64, 1200)])
+def test_a_long_prompt_among_short_ones(kind, B, n, H, heads, hd, L):
+    """The key splits go to the prompts by their lengths: one long, others short or empty, without nodes, or past what
+    the table holds (NaN); rows behind a prompt's nodes stay as they were."""
+    from paper_2412_10418_amd import binding as bd
+    rng = np.random.default_rng([B, n, L])
+    lens = rng.integers(0, 70, B).tolist()
+    at = int(rng.integers(0, B))
+    lens[at] = L
+    nodes = np.full(B, n)
+    if B > 2:
+        lens[(at + 1) % B], nodes[(at + 1) % B] = 0, 0
+        lens[(at + 2) % B] = 0
+    assert bd.lib().cdsl_op_tree_attention_workspace(B, n, H, heads, hd, L) > 0
+    cache, k, v = _filled(rng, B, lens, n, heads, hd, "int8")
+    q = _rows(rng, (B, n, H, hd), "f32").to(KIND[kind])
+    parents = np.stack([random_tree(rng, n, 3) for _ in range(B)])
+    long = lens.copy()
+    over = (at + 3) % B if B > 3 else None
+    if over is not None:
+        long[over] = cache.table.shape[1] * 32 - n + 1
+    for given in (lens, long):
+        out = torch.full_like(q, 7.0)
+        bd.cdsl_op_tree_attention(cache, q, _ints(given), _ints(parents), n_nodes=_ints(nodes), max_len=L, out=out)
+        some = [b for b in sorted({0, at, (at + 1) % B, (at + 2) % B, B - 1}) if given[b] == lens[b]]
+        _check(out[some], q[some], k[some], v[some], [lens[b] for b in some], parents[some], nodes[some].tolist(),
+               hd ** -0.5, f"{kind} at {at}")
+        for b in range(B):
+            assert bool((out[b, nodes[b]:] == 7).all())
+            if given[b] == lens[b]:
+                assert torch.isfinite(out[b, :nodes[b]]).all()
+            else:
+                assert torch.isnan(out[b, :nodes[b]]).all()
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("hd,n,causal", [(128, 64, False), (64, 61, True), (32, 64, False)])
