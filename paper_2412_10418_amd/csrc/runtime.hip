@@ -1982,7 +1982,7 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, 
     if ((long long)n * H > (1 << 30)) return fail(nullptr, CDSL_ERANGE, "n * H exceeds 2^30");
     if (cache->batch == 0 || n == 0) return CDSL_OK;
     const TreeAttnPlan p = tree_attn_plan(cache->batch, n, H, cache->n_kv_heads, cache->head_dim, std::max(max_len, 0));
-    if ((long long)p.row_groups * p.nsplit * cache->batch * cache->n_kv_heads > kMaxGroups ||
+    if ((long long)p.row_groups * p.slots * cache->n_kv_heads > kMaxGroups ||
         (long long)cache->batch * n * H > kMaxGroups)
       return fail(nullptr, CDSL_ERANGE, "too many rows");
     if (p.workspace > 0 && (!workspace || workspace_bytes < p.workspace))

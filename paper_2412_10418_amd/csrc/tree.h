@@ -36,9 +36,9 @@ struct TreeAttnArgs {
   const int* parents;      // null: causal
   int n, H, G;
   float scale_log2;        // softmax scale * log2(e)
-  float* part_o;           // [B nsplit][n * H][hd]
-  float* part_ml;          // [B nsplit][n * H][2]
-  int nsplit, row_groups;  // key splits of a prompt, of all prompts / B
+  float* part_o;           // [slots][n * H][hd]
+  float* part_ml;          // [slots][n * H][2]
+  int slots, row_groups;   // key splits of all prompts (B: no splits)
   int split_pages;         // pages per key split, at least
   int wg_tiles;            // row tiles (of 16) per workgroup
 };
@@ -47,7 +47,7 @@ struct TreeAttnPlan {
   int few;                 // 1, 2: tree_few_kernel with so many row tiles
   bool wide;               // tree_wide_kernel; else tree_many_kernel
   int wg_tiles;            // row tiles (of 16) per workgroup
-  int row_groups, nsplit, split_pages;
+  int row_groups, slots, split_pages;
   size_t workspace;
 };
 

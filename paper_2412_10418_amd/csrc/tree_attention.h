@@ -134,15 +134,33 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x121, 0xF, 0xF, true));
 }
 
-// Key splits of a batch of 2 to 64 prompts.  The launch has room for B nsplit of
-// them; a prompt takes a share in proportion to its pages (its "parts", one at
-// least, of a.split_pages pages or more), so that a long prompt among short
+// The sum over the lanes before this one.
+__device__ __forceinline__ int lanes_before(int v) {
+  int s = v;
+  s += __builtin_amdgcn_update_dpp(0, s, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8 ...
+  s += __builtin_amdgcn_update_dpp(0, s, 0x112, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x114, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x118, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x142, 0xA, 0xF, false);   // ... and the sums of the rows before
+  s += __builtin_amdgcn_update_dpp(0, s, 0x143, 0xC, 0xF, false);
+  return s - v;
+}
+
+// Key splits of a batch of 2 to 64 prompts.  The launch has room for a.slots
+// of them; a prompt takes a share in proportion to its pages (its "parts", one
+// at least, of a.split_pages pages or more), so that a long prompt among short
 // ones does not hold up the rest (8 prompts of up to 32768 tokens: 75 -> 69 us;
-// one of 16384 among 31 of 512: 60 -> 24).  Lane j of a wave finds the parts of prompt
-// j.  ceil(w x) parts of weights w come to at most x sum(w) + B, so the last
-// of the four x fits; the first that does is taken.  (Weights up to 2^25 and
-// 1e-5 under the bound: far more than the rounding of these sums.)
-__device__ __forceinline__ int tree_parts(const TreeAttnArgs& a, int lane) {
+// one of 16384 among 31 of 512: 60 -> 24).  Lane j of a wave finds the parts of
+// prompt j, their size and the slot of the first.
+//
+// ceil(w x) parts of weights w come to at most x sum(w) + B, so the last of the
+// four x fits; the first that does is taken.  (Weights up to 2^25 and 1e-5
+// under the bound: far more than the rounding of these sums.)
+struct TreeParts {
+  int parts, slot;
+  float size;
+};
+__device__ __forceinline__ TreeParts tree_parts(const TreeAttnArgs& a, int lane) {
   const int B = a.c.B;
   float w = 0.f;
   if (lane < B) {
@@ -150,16 +168,24 @@ __device__ __forceinline__ int tree_parts(const TreeAttnArgs& a, int lane) {
     const long long toks = (long long)L + nb;
     if (toks <= (long long)a.c.table_stride * kPage) w = (float)min((toks + kPage - 1) / kPage, 1ll << 25);
   }
-  const float room = (float)(B * a.nsplit), per = 0.99999f / fmaxf(lanes_sum(w), 1.f);
-  const float most = 1.f / (float)a.split_pages;
-  float k[4], sum[4];
+  int parts = 1;
+  float size = w;
+  if (a.slots > B) {
+    const float room = (float)a.slots, per = 0.99999f / fmaxf(lanes_sum(w), 1.f);
+    const float most = 1.f / (float)a.split_pages;
+    float k[4], sum[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float x = fminf((room - (float)(B * i) / 3.f) * per, most);
-    k[i] = lane < B ? fminf(fmaxf(ceilf(w * x), 1.f), (float)kTreeMaxSplits) : 0.f;
-    sum[i] = lanes_sum(k[i]);
+    for (int i = 0; i < 4; ++i) {
+      const float x = fminf((room - (float)(B * i) / 3.f) * per, most);
+      k[i] = lane < B ? fminf(fmaxf(ceilf(w * x), 1.f), (float)kTreeMaxSplits) : 0.f;
+      sum[i] = lanes_sum(k[i]);
+    }
+    const float of = sum[0] <= room ? k[0] : sum[1] <= room ? k[1] : sum[2] <= room ? k[2] : k[3];
+    parts = (int)of;
+    size = w / of;
   }
-  return (int)(sum[0] <= room ? k[0] : sum[1] <= room ? k[1] : sum[2] <= room ? k[2] : k[3]);
+  if (lane >= B) parts = 0;
+  return {parts, lanes_before(parts), size};
 }
 
 // The prompt, KV head, keys and rows of a workgroup that takes `tiles` row
@@ -187,34 +213,32 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs& a, int tiles) 
   const int lane = threadIdx.x & 63, B = a.c.B;
   t.slot = chunk / a.c.Hkv;
   t.kvh = chunk % a.c.Hkv;
-  t.b = t.slot / a.nsplit;
-  t.parts = a.nsplit;
-  int part = t.slot % a.nsplit;
+  t.parts = a.slots / B;
+  t.b = t.slot / t.parts;
+  int part = t.slot % t.parts;
   bool spare = false;
-  if (B > 1 && B <= kTreeShared && a.nsplit > 1) {
-    const int k = tree_parts(a, lane);
-    int base = 0;
-    spare = true;
-    for (int j = 0; j < B; ++j) {
-      const int kj = __builtin_amdgcn_readlane(k, j);
-      if (spare && t.slot < base + kj) {
-        t.b = j;
-        t.parts = kj;
-        part = t.slot - base;
-        spare = false;
+  if (B > 1 && B <= kTreeShared) {
+    const TreeParts p = tree_parts(a, lane);
+    int place = p.slot;
+    if (a.slots < 2 * B) {
+      // Parts of unlike sizes: the largest first, so that the last workgroups
+      // to start are short (12 trees of 65 at 8192: 232 -> 202 us).  The last
+      // six bits of a size make way for the prompt: no two are the same.
+      const int key = (__float_as_int(p.size) & ~63) | (63 - lane);
+      place = 0;
+      if (a.slots == B) {
+        for (int j = 0; j < B; ++j) place += __builtin_amdgcn_readlane(key, j) > key ? 1 : 0;
+      } else {
+        for (int j = 0; j < B; ++j)
+          place += __builtin_amdgcn_readlane(key, j) > key ? __builtin_amdgcn_readlane(p.parts, j) : 0;
       }
-      base += kj;
     }
-  } else if (B > 1 && B <= kTreeShared) {
-    // Prompts of unlike lengths: the longest first, so that the last workgroups
-    // to start are short (one lane a prompt finds its place).
-    const int len = lane < B ? a.lens[lane] : 0;
-    int place = 0;
-    for (int j = 0; j < B; ++j) {
-      const int l = __builtin_amdgcn_readlane(len, j);
-      place += l > len || (l == len && j < lane) ? 1 : 0;
-    }
-    t.b = __builtin_ctzll(__ballot(lane < B && place == t.b));
+    const unsigned long long mine = __ballot(t.slot >= place && t.slot < place + p.parts);
+    spare = mine == 0;
+    t.b = spare ? 0 : __builtin_ctzll(mine);
+    t.parts = __builtin_amdgcn_readlane(p.parts, t.b);
+    part = t.slot - __builtin_amdgcn_readlane(place, t.b);
+    t.slot = __builtin_amdgcn_readlane(p.slot, t.b) + part;
   }
   t.nb = a.n_nodes ? min(max(a.n_nodes[t.b], 0), a.n) : a.n;
   t.nrows = t.nb * a.G;
@@ -1023,12 +1047,12 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeAttnArgs a) {
   const int per_b = a.n * a.H, b = (int)(row / per_b), at = (int)(row % per_b);
   if (a.n_nodes && at / a.H >= a.n_nodes[b]) return;
   // its prompt's splits (tree_span)
-  int ns = a.nsplit, slot = b * a.nsplit;
+  int ns = a.slots / a.c.B, slot = b * ns;
   if (a.c.B > 1 && a.c.B <= kTreeShared) {
-    const int k = tree_parts(a, lane);
-    ns = __builtin_amdgcn_readlane(k, b);
+    const TreeParts p = tree_parts(a, lane);
+    ns = __builtin_amdgcn_readlane(p.parts, b);
     if (ns == 1) return;   // written by tree_*_kernel
-    slot = (int)lanes_sum(lane < b ? (float)k : 0.f);
+    slot = __builtin_amdgcn_readlane(p.slot, b);
   }
   const long long part = (long long)slot * per_b + at;
   constexpr int PER = (HD + 63) / 64;
@@ -1069,13 +1093,13 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeAttnArgs a) {
 
 template <int HD, int FMT, typename QT>
 hipError_t tree_attn_rows(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t st) {
-  const unsigned grid = (unsigned)((long long)p.row_groups * p.nsplit * a.c.B * a.c.Hkv);
+  const unsigned grid = (unsigned)((long long)p.row_groups * p.slots * a.c.Hkv);
   if (p.few == 1) tree_few_kernel<HD, FMT, QT, 1><<<grid, 256, 0, st>>>(a);
   else if (p.few == 2) tree_few_kernel<HD, FMT, QT, 2><<<grid, 256, 0, st>>>(a);
   else if (!p.wide) tree_many_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
   else tree_wide_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.nsplit == 1) return e;
+  if (e != hipSuccess || p.slots == a.c.B) return e;
   const long long rows = (long long)a.c.B * a.n * a.H;
   tree_combine_kernel<HD, QT><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a);
   return hipGetLastError();

@@ -25,32 +25,36 @@ TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len) {
   const int most_tiles = p.few ? p.few : p.wide ? 8 : 4;
   p.row_groups = (tiles + most_tiles - 1) / most_tiles;
   p.wg_tiles = (tiles + p.row_groups - 1) / p.row_groups;
-  // Keys are split until there are two workgroups a CU (few rows) or three,
-  // each with eight pages (few rows: two a wave) or four at least.  More and
-  // smaller splits start more often than they balance (at 512, 768 and 1024
+  // Keys are split until there are two workgroups a CU (few rows) or three, in
+  // parts of eight pages (few rows: two a wave) or four at least.  More and
+  // smaller parts start more often than they balance (at 512, 768 and 1024
   // workgroups: 32 prompts of one token at 4096: 38, 38, 42 us; 8 trees of 65 at
-  // 8192: 248, 151, 153; 4 of 40 at 4000: 34.6, 32.7, 38.8).  Few rows over a
-  // long cache are split in two all the same: one prompt of 16384 among 63 short
-  // ones takes 37 us instead of 116, 64 of 16384 take 378 instead of 372.
-  const long long wgs = pairs * (p.few ? 1 : one);
-  const long long pages = ((long long)max_len + n + kPage - 1) / kPage;
+  // 8192: 248, 151, 153; 4 of 40 at 4000: 34.6, 32.7, 38.8).  Less than two
+  // parts a prompt only where prompts are long and 1.5 are to be had (12 trees
+  // of 65: at 8192 198 us instead of 252, at 2048 72 either way; 16 of 51 at 256:
+  // 45 instead of 28).  Few rows over a long cache are split in two whatever
+  // their number: one prompt of 16384 among 63 short ones takes 37 us instead of
+  // 116, 64 of up to 8192 115 instead of 119.
   p.split_pages = p.few ? 8 : 4;
-  const long long most = std::max<long long>(1, pages / p.split_pages);
-  const long long least = p.few && B > 1 && B <= kTreeShared && pages >= 256 ? 2 : 1;
-  const long long want = std::max<long long>(least, (p.few ? 512 : 768) / std::max<long long>(wgs, 1));
-  p.nsplit = (int)std::min<long long>({want, most, kTreeMaxSplits});
-  p.workspace = p.nsplit > 1 ? (size_t)p.nsplit * B * n * H * (hd + 2) * sizeof(float) : 0;
+  const long long pages = ((long long)max_len + n + kPage - 1) / kPage;
+  const long long most = std::min<long long>(std::max<long long>(1, pages / p.split_pages), kTreeMaxSplits);
+  const bool shared = B > 1 && B <= kTreeShared;
+  long long slots = (p.few ? 512 : 768) / (Hkv * (p.few ? 1 : one));
+  if (p.few && shared && pages >= 256) slots = std::max(slots, 2ll * B);
+  if (!shared || slots < 2 * B && (pages < 128 || 2 * slots < 3 * B)) slots -= slots % B;
+  p.slots = (int)std::max<long long>(B, std::min(slots, B * most));
+  p.workspace = p.slots > B ? (size_t)p.slots * n * H * (hd + 2) * sizeof(float) : 0;
   return p;
 }
 
 hipError_t tree_attn_launch(TreeAttnArgs a, const TreeAttnPlan& p, int dtype, void* workspace, hipStream_t st) {
   if (a.c.B == 0 || a.n == 0) return hipSuccess;
-  a.nsplit = p.nsplit;
+  a.slots = p.slots;
   a.row_groups = p.row_groups;
   a.split_pages = p.split_pages;
   a.wg_tiles = p.wg_tiles;
   a.part_o = (float*)workspace;
-  a.part_ml = a.part_o + (size_t)p.nsplit * a.c.B * a.n * a.H * a.c.hd;
+  a.part_ml = a.part_o + (size_t)p.slots * a.n * a.H * a.c.hd;
   switch (a.c.hd) {
     case 32: return tree_attn_hd32(a, p, dtype, st);
     case 64: return tree_attn_hd64(a, p, dtype, st);
