@@ -270,10 +270,10 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_read_kernel(KvqView c, 
 // Moves of single tokens: their bytes lie in 16 lines of the keys and all 32
 // of the values, as the attention's order has it, so the lines and not the
 // bytes bound it (16 prompts x 8 tokens x 256 units of hd = 128: 17 MB of
-// tokens, 17 us).  One wave per (layer, KV head, prompt).  Entry i of the path moves from
-// slot L + path[i] to L + i.  Eight entries at a time are read before any of
-// them is written; with path ascending, path[i] >= i, so that no later
-// entry's source has been written by then.
+// tokens, 17 us).  One wave per (layer, KV head, prompt).  Entry i of the path
+// moves from slot L + path[i] to L + i.  Eight entries at a time are read
+// before any of them is written; with path ascending, path[i] >= i, so that no
+// later entry's source has been written by then.
 template <int HD>
 __global__ __launch_bounds__(64) void kvq_keep_kernel(KvqView c, long long layer_bytes, const int* lens,
                                                       const int* path, const int* n_path, int n, int* new_lens) {

@@ -104,7 +104,8 @@ __device__ __forceinline__ unsigned byte_mask(unsigned m) {
   return ((m & 1u) | (m & 2u) << 7 | (m & 4u) << 14 | (m & 8u) << 21) * 255u;
 }
 
-// e4m3 codes of slots past the last node (never written) may be NaNs: zeros.
+// e4m3 codes of slots past the last node (never written), and those read in
+// place of a page that does not exist (held = 0), may be NaNs: zeros.
 __device__ __forceinline__ u32x4 hold_values(u32x4 w, int held, int lg) {
   const unsigned hm = held >= 32 ? ~0u : (1u << held) - 1u;
   const unsigned mA = byte_mask(hm >> (4 * lg)), mB = byte_mask(hm >> (16 + 4 * lg));
@@ -580,7 +581,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
     }
     if constexpr (FMT == kE4M3 && MASKED) {
 #pragma unroll
-      for (int s = 0; s < S; ++s) vr[s] = hold_values(vr[s], t.L + t.nb - page * kPage, lg);
+      for (int s = 0; s < S; ++s) vr[s] = hold_values(vr[s], bad ? 0 : t.L + t.nb - page * kPage, lg);
     }
     // The next page's loads are in flight during the rest: all of them where
     // there is room for this page's values as bf16, else its keys'.
@@ -726,7 +727,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void t
         y.h = codes_f16<FMT>(w.z, w.w);
       } else {
         u32x4 v = w;
-        if (FMT == kE4M3 && (page + 1) * kPage > t.L) v = hold_values(v, t.L + t.nb - page * kPage, lg);
+        if (FMT == kE4M3 && (page + 1) * kPage > t.L) v = hold_values(v, bad[buf] ? 0 : t.L + t.nb - page * kPage, lg);
         x.b = codes_bf16<FMT>(v.x, v.y);
         y.b = codes_bf16<FMT>(v.z, v.w);
       }
@@ -873,7 +874,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
         at[16] = k1.u;
       } else {   // dims 32 d + x and + 16, slots 4 g .. +3 and 16 + 4 g .. +3
         u32x4 v = w;
-        if (FMT == kE4M3 && (page + 1) * kPage > t.L) v = hold_values(v, t.L + t.nb - page * kPage, g);
+        if (FMT == kE4M3 && (page + 1) * kPage > t.L) v = hold_values(v, bad[buf] ? 0 : t.L + t.nb - page * kPage, g);
         union {
           bf16x8 b8;
           uint2 u[2];

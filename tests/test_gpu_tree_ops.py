@@ -365,6 +365,35 @@ def test_nan_rows_and_missing_pages_reach_the_rows_that_see_them():
     assert torch.isnan(long[0]).all() and torch.isnan(long[2]).all() and not torch.isnan(long[3]).any()
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,H,heads", [(1, 14, 2, 2), (2, 24, 2, 2), (2, 24, 8, 2), (100, 64, 16, 8)])
+def test_a_missing_page_spares_the_rows_that_do_not_see_it(fmt, kind, B, n, H, heads):
+    """A star whose nodes from 12 on lie on a page that the pool does not have, in a pool of NaN codes and scales."""
+    from paper_2412_10418_amd import binding as bd
+    rng = np.random.default_rng([n, H])
+    L, hd = 20, 64
+    cache = paged(rng, 1, B, L + n, heads, hd, fmt, fill=0xFF)
+    table = cache.table.clone()
+    table[table == 0] = next(i for i in range(cache.pool.shape[1]) if i not in set(table.flatten().tolist()))
+    cache = bd.QuantCache(cache.pool, table, hd, fmt)
+    K, V = _rows(rng, (B, L + n, heads, hd), kind), _rows(rng, (B, L + n, heads, hd), kind)
+    bd.cdsl_op_kvq_write(cache, K, V)
+    k, v = bd.cdsl_op_kvq_read(cache, L + n)
+    k, v = _np(k).astype(np.float64), _np(v).astype(np.float64)
+    q = _rows(rng, (B, n, H, hd), kind)
+    parents = np.stack([random_tree(rng, n, 3, "star")] * B)
+    whole = table[:, 1].clone()
+    for missing in (-1, cache.pool.shape[1]):
+        table[:, 1] = missing
+        out = bd.cdsl_op_tree_attention(cache, q, _ints([L] * B), _ints(parents))
+        on_it = torch.arange(n, device="cuda").add(L).floor_divide(32) == 1
+        assert torch.isnan(out[:, on_it]).all() and torch.isfinite(out[:, ~on_it]).all()
+        _check(out[:2, :12], q[:2, :12], k, v, [L] * min(B, 2), parents[:, :12], [12] * min(B, 2), hd ** -0.5, f"{fmt} {kind}")
+    table[:, 1] = whole
+    assert torch.isfinite(bd.cdsl_op_tree_attention(cache, q, _ints([L] * B), _ints(parents))).all()
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_scores_far_apart_and_scales(kind):
     """Sharp softmaxes (scores to some hundreds), a zero and a negative scale, and values of unlike sizes."""
