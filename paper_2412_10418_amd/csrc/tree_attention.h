@@ -20,7 +20,9 @@
 // Probabilities times s_v can be of any size, so they stay bf16: three planes
 // (their 24 bits) for fp32, one (2^-8 of each, independent over the keys; the
 // result rounds by as much) for bf16.  Two planes would lose 2^-16 of each
-// probability: 2.5e-6 of the result, where fp32 products give 0.8e-6.
+// probability: 2.5e-6 of the result, where fp32 products give 0.8e-6.  (A
+// second plane for bf16 would bring 0.0017 of the result instead of 0.0023, for
+// 10% more time where there are many rows.)
 //
 // Three kernels.  Few rows (one or two tiles): the codes go from memory
 // straight to the registers of the wave that uses them, and the waves of a
@@ -668,8 +670,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
 // wave w takes tile w.  A page is converted once for all waves: its
 // codes come in as 16 bytes a thread, two pages before they are needed, and go
 // to LDS as f16 (keys) and bf16 (values) in operand order.
-template <int HD, int FMT, typename QT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void tree_many_kernel(TreeAttnArgs a) {
+// EU: waves a SIMD at least.  Four leave 128 registers a lane (the loop likes
+// 132 in bf16, 146 in fp32, a few of which then live in scratch outside it).
+template <int HD, int FMT, typename QT, int EU>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EU))) void tree_many_kernel(TreeAttnArgs a) {
   using Row = RowTile<HD, QT>;
   constexpr int NT = 256, W = 4;
   constexpr int S = Row::S, DT = Row::DT;
@@ -811,8 +815,9 @@ struct WideTile {
 // where each alone takes 250), and the vector work of the softmax is as long
 // as the products.  Executed products: 0.96 PFLOP/s in fp32 (40 instructions a
 // tile and page; 64 prompts x 8 KV heads of 16 tiles at 1024 tokens), 1.19 (8 x
-// 8 of 128 tiles, causal), where a product of 8192^3 reaches 1.40.  Scores: lane (row, h) holds slots 8 j + 4 h + e, j < 4, e < 4,
-// which in that order are its operand of the two value products of 16 slots.
+// 8 of 128 tiles, causal), where a product of 8192^3 reaches 1.40.
+// Scores: lane (row, h) holds slots 8 j + 4 h + e, j < 4, e < 4, which in that
+// order are its operand of the two value products of 16 slots.
 template <int HD, int FMT, typename QT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void tree_wide_kernel(TreeAttnArgs a) {
   using Row = WideTile<HD, QT>;
@@ -1097,8 +1102,14 @@ hipError_t tree_attn_rows(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStrea
   const unsigned grid = (unsigned)((long long)p.row_groups * p.slots * a.c.Hkv);
   if (p.few == 1) tree_few_kernel<HD, FMT, QT, 1><<<grid, 256, 0, st>>>(a);
   else if (p.few == 2) tree_few_kernel<HD, FMT, QT, 2><<<grid, 256, 0, st>>>(a);
-  else if (!p.wide) tree_many_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
-  else tree_wide_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
+  else if (!p.wide) {
+    // Four workgroups a CU where there are as many; fewer are faster in three (64
+    // trees of 65 at 2048 in bf16: 152 -> 146 us; 16 of them: 56 -> 61).  Heads
+    // of 64 gain nothing by it, fp32 over int8 loses 5% (231 -> 243).
+    constexpr bool kFour = HD == 128 && (sizeof(QT) == 2 || FMT == kE4M3);
+    if (kFour && grid >= 1024) tree_many_kernel<HD, FMT, QT, kFour ? 4 : 3><<<grid, 256, 0, st>>>(a);
+    else tree_many_kernel<HD, FMT, QT, 3><<<grid, 256, 0, st>>>(a);
+  } else tree_wide_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == a.c.B) return e;
   const long long rows = (long long)a.c.B * a.n * a.H;
