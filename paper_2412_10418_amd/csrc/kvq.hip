@@ -9,6 +9,8 @@
 // A row that holds a NaN or an infinity has s = NaN and codes 0: it reads
 // back as NaN.  Scales stay fp32, so that a value differs from its input by
 // its code's rounding alone.
+#include <type_traits>
+
 #include "tree.h"
 
 namespace cdsl {
@@ -41,21 +43,34 @@ __device__ __forceinline__ unsigned encode4(const float (&x)[4], float s) {
     w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, w, true);
     return w;
   } else {
-    // The product with an approximate 1 / s is off by less than 2^-14, so
-    // its integer is the nearest one to x / s or next to it; the signs of
+    // 1 / s to 2^-23 of itself by one Newton step, so that x / s <= 127.5 is off
+    // by less than 2^-15: the nearest integer is the right one unless x / s
+    // lies as near to a tie.  There (once in 2^14 values) the signs of
     // x - s (n +- 1/2), which one fused multiply-add gives exactly, tell.
-    const float inv = __builtin_amdgcn_rcpf(s);
-    unsigned w = 0;
+    float inv = __builtin_amdgcn_rcpf(s);
+    inv = fmaf(inv, fmaf(-s, inv, 1.f), inv);
+    float n[4], far = 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float n = __builtin_rintf(x[e] * inv);
-      const float up = fmaf(-s, n + 0.5f, x[e]), dn = fmaf(-s, n - 0.5f, x[e]);
-      const bool odd = (int)n & 1;
-      if (up > 0.f || (up == 0.f && odd)) n += 1.f;
-      else if (dn < 0.f || (dn == 0.f && odd)) n -= 1.f;
-      w |= ((unsigned)(int)n & 255u) << (8 * e);
+      const float r = x[e] * inv;
+      n[e] = __builtin_rintf(r);
+      far = fmaxf(far, fabsf(r - n[e]));
     }
-    return w;
+    if (far > 0.5f - 0x1p-14f) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float up = fmaf(-s, n[e] + 0.5f, x[e]), dn = fmaf(-s, n[e] - 0.5f, x[e]);
+        const bool odd = (int)n[e] & 1;
+        if (up > 0.f || (up == 0.f && odd)) n[e] += 1.f;
+        else if (dn < 0.f || (dn == 0.f && odd)) n[e] -= 1.f;
+      }
+    }
+    // 1.5 2^23 + n has n in its low bits
+    unsigned u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(n[e] + 0x1.8p23f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400), __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400),
+                                 0x05040100);
   }
 }
 
@@ -67,7 +82,11 @@ __device__ __forceinline__ float scale_of(float a) {
     const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
     return __uint_as_float((unsigned)max(e, 1) << 23);
   } else {
-    return fmaxf(a / 127.f, 1.1754943508222875e-38f);
+    // a / 127 rounded to nearest: with the rounded reciprocal, one correction
+    // by the exact remainder gives it (Markstein 1990; checked for every a)
+    constexpr float y = 1.f / 127.f;
+    const float t = a * y;
+    return fmaxf(fmaf(fmaf(-127.f, t, a), y, t), 1.1754943508222875e-38f);
   }
 }
 
@@ -128,7 +147,10 @@ template <int HD>
 constexpr int kvq_threads() { return 4 * HD < 256 ? 4 * HD : 256; }
 
 // Workgroup = (page of the prompt's run, KV head, prompt).  The bytes of the
-// rows bound it (in fp32 they are 4 of every 5 bytes moved).
+// rows bound it (in fp32 they are 4 of every 5 bytes moved): 16 prompts of 256
+// x 32 heads of 128 in fp32 take 29.6 us, 5.7 TB/s with what the last cache holds,
+// 24 of up to 2047 x 8 in bf16 32.0.  Branches for every row and tie, rather than
+// for the page and four values, cost 5 and 10 us.
 template <int HD, int FMT, typename T>
 __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_write_kernel(KvqView c, KvqRows r) {
   constexpr int NT = kvq_threads<HD>();
@@ -143,68 +165,73 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_write_kernel(KvqView c,
   if (base >= end || base + kPage <= beg) return;
   uint8_t* unit = kvq_unit_of(c, b, page, h);
   if (!unit) return;
-  const bool whole = base >= beg && base + kPage <= end;
-  float x[PER][4][4];
+  // whole pages go through LDS, so that their lines leave whole; of the others
+  // only the run's bytes are written
+  auto page_rows = [&](auto all) __attribute__((always_inline)) {
+    constexpr bool WHOLE = decltype(all)::value;
+    float x[PER][4][4];
 #pragma unroll
-  for (int u = 0; u < PER; ++u) {
-    const int task = threadIdx.x + NT * u;
-    const int isv = task / (8 * LQ), quad = task / LQ % 8, d = task % LQ * 4;
-    const T* src = (const T*)(isv ? r.V : r.K) + (isv ? r.vsb : r.ksb) * b + h * HD + d;
-    const long long ts = isv ? r.vst : r.kst;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const long long pos = base + 4 * quad + t;
-      if (pos >= beg && pos < end) load4<T>(src + (pos - beg) * ts, x[u][t]);
-      else x[u][t][0] = x[u][t][1] = x[u][t][2] = x[u][t][3] = 0.f;
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < PER; ++u) {
-    const int task = threadIdx.x + NT * u;
-    const int isv = task / (8 * LQ), quad = task / LQ % 8, d = task % LQ * 4;
-    float s[4];
-    unsigned w[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      // the largest bit pattern of |x|: NaN and infinity stay on top
-      unsigned a = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) a = max(a, __float_as_uint(x[u][t][e]) & 0x7fffffffu);
-      a = group_max<LQ>(a);
-      const bool bad = a >= 0x7f800000u;
-      s[t] = bad ? __uint_as_float(0x7fc00000u) : scale_of<FMT>(__uint_as_float(a));
-      w[t] = bad ? 0u : encode4<FMT>(x[u][t], s[t]);
-    }
-    const int slot = 4 * quad;
-    float* sc = (float*)(unit + (isv ? kvq_value_scale_at(HD, slot) : kvq_key_scale_at(HD, slot)));
-    if (d == 0) {
-      if (whole) *(f32x4*)sc = (f32x4){s[0], s[1], s[2], s[3]};
-      else
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (base + slot + t >= beg && base + slot + t < end) sc[t] = s[t];
-    }
-    unsigned o[4];
-    if (isv) transpose4(w, o);
-    if (whole) {
+    for (int u = 0; u < PER; ++u) {
+      const int task = threadIdx.x + NT * u;
+      const int isv = task / (8 * LQ), quad = task / LQ % 8, d = task % LQ * 4;
+      const T* src = (const T*)(isv ? r.V : r.K) + (isv ? r.vsb : r.ksb) * b + h * HD + d;
+      const long long ts = isv ? r.vst : r.kst;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        if (isv) lds[banked(kvq_value_at(HD, slot, d + t) / 4)] = o[t];
-        else lds[banked(kvq_key_at(slot + t, d) / 4)] = w[t];
-      }
-    } else {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const bool live = base + slot + t >= beg && base + slot + t < end;
-        if (!live) continue;
-        if (!isv) *(unsigned*)(unit + kvq_key_at(slot + t, d)) = w[t];
-        else
-#pragma unroll
-          for (int e = 0; e < 4; ++e) unit[kvq_value_at(HD, slot + t, d + e)] = (uint8_t)(w[t] >> (8 * e));
+        const long long pos = base + 4 * quad + t;
+        if (WHOLE || (pos >= beg && pos < end)) load4<T>(src + (pos - beg) * ts, x[u][t]);
+        else x[u][t][0] = x[u][t][1] = x[u][t][2] = x[u][t][3] = 0.f;
       }
     }
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int task = threadIdx.x + NT * u;
+      const int isv = task / (8 * LQ), quad = task / LQ % 8, d = task % LQ * 4;
+      float s[4];
+      unsigned w[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        // the largest bit pattern of |x|: NaN and infinity stay on top
+        unsigned a = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a = max(a, __float_as_uint(x[u][t][e]) & 0x7fffffffu);
+        a = group_max<LQ>(a);
+        const bool bad = a >= 0x7f800000u;
+        s[t] = scale_of<FMT>(__uint_as_float(a));
+        w[t] = encode4<FMT>(x[u][t], s[t]);
+        s[t] = bad ? __uint_as_float(0x7fc00000u) : s[t];
+        w[t] = bad ? 0u : w[t];
+      }
+      const int slot = 4 * quad;
+      float* sc = (float*)(unit + (isv ? kvq_value_scale_at(HD, slot) : kvq_key_scale_at(HD, slot)));
+      if constexpr (WHOLE) {
+        if (d == 0) *(f32x4*)sc = (f32x4){s[0], s[1], s[2], s[3]};
+        unsigned o[4];
+        if (isv) transpose4(w, o);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          if (isv) lds[banked(kvq_value_at(HD, slot, d + t) / 4)] = o[t];
+          else lds[banked(kvq_key_at(slot + t, d) / 4)] = w[t];
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const bool live = base + slot + t >= beg && base + slot + t < end;
+          if (!live) continue;
+          if (d == 0) sc[t] = s[t];
+          if (!isv) *(unsigned*)(unit + kvq_key_at(slot + t, d)) = w[t];
+          else
+#pragma unroll
+            for (int e = 0; e < 4; ++e) unit[kvq_value_at(HD, slot + t, d + e)] = (uint8_t)(w[t] >> (8 * e));
+        }
+      }
+    }
+  };
+  if (base < beg || base + kPage > end) {   // uniform over the workgroup
+    page_rows(std::false_type{});
+    return;
   }
-  if (!whole) return;   // uniform over the workgroup
+  page_rows(std::true_type{});
   __syncthreads();
 #pragma unroll
   for (int i = threadIdx.x; i < 2 * kPage * HD / 16; i += NT) *((u32x4*)unit + i) = *(const u32x4*)&lds[banked(4 * i)];
