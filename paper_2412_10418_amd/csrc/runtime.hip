@@ -1959,7 +1959,7 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V, int
 size_t cdsl_op_tree_attention_workspace(int32_t batch, int32_t n, int32_t H, int32_t n_kv_heads, int32_t head_dim,
                                         int32_t max_len) {
   if (batch <= 0 || n <= 0 || H <= 0 || n_kv_heads <= 0 || H % n_kv_heads != 0 || (long long)n * H > (1 << 30)) return 0;
-  return tree_attn_plan(batch, n, H, n_kv_heads, head_dim, std::max(max_len, 0)).workspace;
+  return tree_attn_plan(batch, n, H, n_kv_heads, head_dim, std::max(max_len, 0), CDSL_F32, CDSL_KVQ_INT8).workspace;
 }
 
 int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, int32_t dtype, int32_t n, int32_t H,
@@ -1981,7 +1981,8 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, 
     if (parents && n > CDSL_TREE_MAX) return fail(nullptr, CDSL_ERANGE, "a tree has at most 512 nodes");
     if ((long long)n * H > (1 << 30)) return fail(nullptr, CDSL_ERANGE, "n * H exceeds 2^30");
     if (cache->batch == 0 || n == 0) return CDSL_OK;
-    const TreeAttnPlan p = tree_attn_plan(cache->batch, n, H, cache->n_kv_heads, cache->head_dim, std::max(max_len, 0));
+    const TreeAttnPlan p = tree_attn_plan(cache->batch, n, H, cache->n_kv_heads, cache->head_dim, std::max(max_len, 0),
+                                          dtype, cache->format);
     if ((long long)p.row_groups * p.slots * cache->n_kv_heads > kMaxGroups ||
         (long long)cache->batch * n * H > kMaxGroups)
       return fail(nullptr, CDSL_ERANGE, "too many rows");

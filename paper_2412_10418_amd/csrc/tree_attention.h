@@ -813,9 +813,8 @@ struct WideTile {
 // issuing vector ones for about eight cycles whatever its size (a wave of
 // either beside a wave of vector work: 376 us for 16x16x32, 326 for 32x32x16,
 // where each alone takes 250), and the vector work of the softmax is as long
-// as the products.  Executed products: 0.96 PFLOP/s in fp32 (40 instructions a
-// tile and page; 64 prompts x 8 KV heads of 16 tiles at 1024 tokens), 1.19 (8 x
-// 8 of 128 tiles, causal), where a product of 8192^3 reaches 1.40.
+// as the products (64 prompts x 8 KV heads of 256 rows at up to 2048 tokens: 119
+// us in bf16, 194 in fp32 over int8, where tiles of 16 take 127 and 201).
 // Scores: lane (row, h) holds slots 8 j + 4 h + e, j < 4, e < 4, which in that
 // order are its operand of the two value products of 16 slots.
 template <int HD, int FMT, typename QT>
@@ -1109,7 +1108,9 @@ hipError_t tree_attn_rows(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStrea
     constexpr bool kFour = HD == 128 && (sizeof(QT) == 2 || FMT == kE4M3);
     if (kFour && grid >= 1024) tree_many_kernel<HD, FMT, QT, kFour ? 4 : 3><<<grid, 256, 0, st>>>(a);
     else tree_many_kernel<HD, FMT, QT, 3><<<grid, 256, 0, st>>>(a);
-  } else tree_wide_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
+  } else if constexpr (tree_may_be_wide(HD, sizeof(QT) == 2, FMT)) {
+    tree_wide_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == a.c.B) return e;
   const long long rows = (long long)a.c.B * a.n * a.H;

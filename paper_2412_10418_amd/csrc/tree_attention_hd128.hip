@@ -10,18 +10,17 @@ hipError_t tree_attn_hd128(const TreeAttnArgs& a, const TreeAttnPlan& p, int dty
   return tree_attn_hd<128>(a, p, dtype, st);
 }
 
-TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len) {
+TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, int dtype, int format) {
   TreeAttnPlan p{};
   const int tiles = (int)(((long long)n * (H / Hkv) + 15) / 16);
   p.few = tiles <= 2 ? tiles : 0;
-  // Tiles of 32 rows take 0.95 (fp32) or 0.85 (bf16) of the time where they
-  // fill the chip (64 prompts x 8 KV heads of 16 tiles of 16 at 1024 tokens: 190
-  // against 202 us, 120 against 138), not where they leave slots empty (17
-  // tiles: 231 against 228) or give less than three workgroups a CU (16 pairs of
-  // 128 tiles: 97 against 82).
+  // Tiles of 32 rows where they fill their workgroups, and those the chip three
+  // times over (64 prompts x 8 KV heads of 16 tiles of 16 at up to 2048 tokens: 119
+  // against 127 us in bf16, 194 against 201 in fp32 over int8; of 14 tiles 75.0
+  // against 74.7, of 17 134 against 125; 16 pairs of 128 tiles 97 against 82).
   const long long pairs = (long long)B * Hkv;
   const long long one = (tiles + 3) / 4, two = (tiles + 7) / 8;
-  p.wide = !p.few && pairs * two >= 768 && 8 * two * 0.93 < 4 * one;
+  p.wide = !p.few && pairs * two >= 768 && 8 * two - tiles <= 1 && tree_may_be_wide(hd, dtype, format);
   const int most_tiles = p.few ? p.few : p.wide ? 8 : 4;
   p.row_groups = (tiles + most_tiles - 1) / most_tiles;
   p.wg_tiles = (tiles + p.row_groups - 1) / p.row_groups;
