@@ -1959,7 +1959,7 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V, int
 size_t cdsl_op_tree_attention_workspace(int32_t batch, int32_t n, int32_t H, int32_t n_kv_heads, int32_t head_dim,
                                         int32_t max_len) {
   if (batch <= 0 || n <= 0 || H <= 0 || n_kv_heads <= 0 || H % n_kv_heads != 0 || (long long)n * H > (1 << 30)) return 0;
-  return tree_attn_plan(batch, n, H, n_kv_heads, head_dim, std::max(max_len, 0), CDSL_F32, CDSL_KVQ_INT8).workspace;
+  return tree_attn_workspace(batch, n, H, n_kv_heads, head_dim, std::max(max_len, 0));
 }
 
 int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, int32_t dtype, int32_t n, int32_t H,

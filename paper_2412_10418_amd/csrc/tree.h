@@ -53,8 +53,8 @@ struct TreeAttnPlan {
 
 // fp32 over e4m3 (heads of 128) is as fast in tiles of 16 rows (188 us) as of 32 (190).
 constexpr bool tree_may_be_wide(int hd, int dtype, int format) { return !(hd == 128 && dtype == 0 && format == kE4M3); }
-// (The workspace does not depend on the types.)
 TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, int dtype, int format);
+size_t tree_attn_workspace(int B, int n, int H, int Hkv, int hd, int max_len);   // enough for every type and format
 hipError_t tree_attn_launch(TreeAttnArgs a, const TreeAttnPlan& p, int dtype, void* workspace, hipStream_t st);
 
 constexpr int kAcceptMaxVocab = 1 << 20;
