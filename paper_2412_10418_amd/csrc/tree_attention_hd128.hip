@@ -23,12 +23,13 @@ TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, i
   //  - where the keys are split anyway, are many, and half the workgroups take
   //    the rows (8 prompts of 17 x 4 rows at 8192: 62 against 68 us in bf16, 85
   //    against 90 in fp32; 32: 184 against 240 and 281 against 331; but 8 of 32 x
-  //    4 at 2048: 36.5 against 35.1).
+  //    4 at 2048: 36.5 against 35.1; one of 61 x 4 at 4096: 27.1 against 24.6; two
+  //    chunks of 509 x 4 at 4000: 121 against 145 in bf16, at 2000: 82 against 79).
   const long long pairs = (long long)B * Hkv;
   const long long one = (tiles + 3) / 4, two = (tiles + 7) / 8, full = pairs * two;
   const long long pages = ((long long)max_len + n + kPage - 1) / kPage;
   const bool filled = 8 * two - tiles <= 1 && (full >= 768 || (dtype == 1 && full >= 448 && full <= 512));
-  const bool split = one == 2 * two && full * 3 <= 512 * 2 && pages >= 128 && pairs * pages >= 8192;
+  const bool split = one == 2 * two && full * 3 <= 512 * 2 && pages >= 128 && full * pages >= 8192;
   p.wide = !p.few && (filled || split) && tree_may_be_wide(hd, dtype, format);
   const int most_tiles = p.few ? p.few : p.wide ? 8 : 4;
   p.row_groups = (tiles + most_tiles - 1) / most_tiles;
