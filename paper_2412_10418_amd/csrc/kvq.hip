@@ -294,25 +294,47 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_read_kernel(KvqView c, 
   }
 }
 
-// Moves of single tokens: their bytes lie in 16 lines of the keys and all 32
-// of the values, as the attention's order has it, so the lines and not the
-// bytes bound it (16 prompts x 8 tokens x 256 units of hd = 128: 17 MB of
-// tokens, 17 us).  One wave per (layer, KV head, prompt).  Entry i of the path
-// moves from slot L + path[i] to L + i.  Eight entries at a time are read
+// The pointer that another lane holds.
+template <typename P>
+__device__ __forceinline__ P* ptr_of_lane(P* p, int lane) {
+  return (P*)__shfl((long long)p, lane, 64);
+}
+
+// Moves of single tokens.  One wave per (layer, KV head, prompt); entry i of the
+// path moves from slot L + path[i] to L + i.  Eight entries at a time are read
 // before any of them is written; with path ascending, path[i] >= i, so that no
 // later entry's source has been written by then.
+//
+// A token's keys lie in hd / 8 runs of 8 bytes: one instruction moves those of
+// several tokens.  Its values lie one byte in eight: a lane reads the 16 bytes
+// around two of them (dims x and x + 16) and collects those of eight tokens; the
+// eight slots that they go to lie in at most three aligned groups of four, so
+// that three reads and three writes of 16 bytes place them all.  (The page is
+// the prompt's own from lens on, so the other bytes may be written back.)  The
+// requests bound it: 16 prompts x 8 tokens x 256 units of hd = 128, 17 MB of
+// tokens, 11.5 us; with a byte at a time 16.5 (64 prompts: 39 and 72).
 template <int HD>
 __global__ __launch_bounds__(64) void kvq_keep_kernel(KvqView c, long long layer_bytes, const int* lens,
                                                       const int* path, const int* n_path, int n, int* new_lens) {
   constexpr int CH = 8;
+  constexpr int KL = HD / 8, TK = 64 / KL < CH ? 64 / KL : CH;   // lanes of a token's keys, tokens at once
+  constexpr int VL = HD / 2, TV = 64 / VL;                       // the same for values
   const int b = blockIdx.y, h = blockIdx.x % c.Hkv, layer = blockIdx.x / c.Hkv;
   const int lane = threadIdx.x;
   c.pool += layer * layer_bytes;
   const int L = max(lens[b], 0);
   const int m = min(max(n_path[b], 0), n);
   if (new_lens && blockIdx.x == 0 && lane == 0) new_lens[b] = L + m;
+  // a lane's 16 bytes of values in the group of four slots that holds `slot`
+  auto values_at = [&](int slot) __attribute__((always_inline)) {
+    const int x = lane % VL;
+    return kPage * HD + x / 16 * 1024 + slot % 16 / 4 * 256 + x % 16 * 16;
+  };
   for (int i0 = 0; i0 < m; i0 += CH) {
-    // lanes 0..7: an entry's source and destination units (null: not moved)
+    // lanes 0..7: an entry's source and destination units (null: not moved);
+    // lanes 8..10: the units of the groups of four that the entries go to
+    const long long first = (long long)L + i0;
+    const int off = (int)(first & 3);
     const uint8_t* src = nullptr;
     uint8_t* dst = nullptr;
     int ss = 0, ds = 0;
@@ -326,40 +348,97 @@ __global__ __launch_bounds__(64) void kvq_keep_kernel(KvqView c, long long layer
         ss = (int)(sp % kPage);
         ds = (int)(dp % kPage);
       }
+    } else if (lane >= CH && lane < CH + 3) {
+      const long long dp = first - off + 4 * (lane - CH);
+      dst = kvq_unit_of(c, b, dp / kPage, h);
+      ds = (int)(dp % kPage);
     }
-    if (!__ballot(src != nullptr)) continue;
-    const uint8_t* su[CH];
-    uint8_t* du[CH];
-    int sl[CH], dl[CH];
+    const unsigned moved = (unsigned)__ballot(src != nullptr);
+    if (!moved) continue;
+
+    uint2 kr[CH / TK];
 #pragma unroll
-    for (int u = 0; u < CH; ++u) {
-      su[u] = (const uint8_t*)__shfl((long long)src, u, 64);
-      du[u] = (uint8_t*)__shfl((long long)dst, u, 64);
-      sl[u] = __shfl(ss, u, 64);
-      dl[u] = __shfl(ds, u, 64);
+    for (int j = 0; j < CH / TK; ++j) {
+      const int e = j * TK + lane / KL;   // (past the eighth: null)
+      const uint8_t* s = ptr_of_lane(src, e);
+      const int slot = __shfl(ss, e, 64);
+      if (s) kr[j] = *(const uint2*)(s + kvq_key_at(slot, lane % KL * 8));
     }
-    uint2 kr[CH];
-    uint8_t vr[CH][(HD + 63) / 64];
-    unsigned sc[CH];
+    float sc = 0.f;
+    {
+      const uint8_t* s = ptr_of_lane(src, lane / 2);
+      const int slot = __shfl(ss, lane / 2, 64);
+      if (s) sc = *(const float*)(s + (lane & 1 ? kvq_value_scale_at(HD, slot) : kvq_key_scale_at(HD, slot)));
+    }
+    u32x4 vr[CH / TV];
 #pragma unroll
-    for (int u = 0; u < CH; ++u) {
-      if (!su[u]) continue;
-      if (lane < HD / 8) kr[u] = *(const uint2*)(su[u] + kvq_key_at(sl[u], 8 * lane));
-      else if (lane < HD / 8 + 2)
-        sc[u] = *(const unsigned*)(su[u] + (lane == HD / 8 ? kvq_key_scale_at(HD, sl[u]) : kvq_value_scale_at(HD, sl[u])));
+    for (int j = 0; j < CH / TV; ++j) {
+      const int e = j * TV + lane / VL;
+      const uint8_t* s = ptr_of_lane(src, e);
+      const int slot = __shfl(ss, e, 64);
+      vr[j] = s ? *(const u32x4*)(s + values_at(slot)) : (u32x4){0u, 0u, 0u, 0u};
+    }
+    // byte e: entry e's value, of dims x and x + 16
+    unsigned long long got[2] = {0, 0};
 #pragma unroll
-      for (int e = 0; e < (HD + 63) / 64; ++e)
-        if (lane + 64 * e < HD) vr[u][e] = su[u][kvq_value_at(HD, sl[u], lane + 64 * e)];
+    for (int j = 0; j < CH / TV; ++j) {
+      const int e = j * TV + lane / VL;
+      const int slot = __shfl(ss, e, 64);
+      got[0] |= (unsigned long long)((slot & 16 ? vr[j].y : vr[j].x) >> (8 * (slot & 3)) & 255u) << (8 * e);
+      got[1] |= (unsigned long long)((slot & 16 ? vr[j].w : vr[j].z) >> (8 * (slot & 3)) & 255u) << (8 * e);
     }
 #pragma unroll
-    for (int u = 0; u < CH; ++u) {
-      if (!su[u]) continue;
-      if (lane < HD / 8) *(uint2*)(du[u] + kvq_key_at(dl[u], 8 * lane)) = kr[u];
-      else if (lane < HD / 8 + 2)
-        *(unsigned*)(du[u] + (lane == HD / 8 ? kvq_key_scale_at(HD, dl[u]) : kvq_value_scale_at(HD, dl[u]))) = sc[u];
+    for (int o = VL; o < 64; o <<= 1)
 #pragma unroll
-      for (int e = 0; e < (HD + 63) / 64; ++e)
-        if (lane + 64 * e < HD) du[u][kvq_value_at(HD, dl[u], lane + 64 * e)] = vr[u][e];
+      for (int k = 0; k < 2; ++k) got[k] |= (unsigned long long)__shfl_xor((long long)got[k], o, 64);
+    // the moved entries' bytes
+    unsigned long long mask = 0;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) mask |= moved >> e & 1u ? 255ull << (8 * e) : 0ull;
+    // their word in group k of four slots: bytes 4 k - off .. + 3
+    auto group = [&](unsigned long long w, int k) __attribute__((always_inline)) {
+      return k == 0 ? (unsigned)w << (8 * off) : k == 1 ? (unsigned)(w >> (32 - 8 * off))
+                                                        : off ? (unsigned)(w >> (64 - 8 * off)) : 0u;
+    };
+    u32x4 old[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const uint8_t* d = ptr_of_lane(dst, CH + k);
+      const int slot = __shfl(ds, CH + k, 64);
+      if (lane < VL && group(mask, k)) old[k] = *(const u32x4*)(d + values_at(slot));
+    }
+
+#pragma unroll
+    for (int j = 0; j < CH / TK; ++j) {
+      const int e = j * TK + lane / KL;
+      const bool live = ptr_of_lane(src, e) != nullptr;
+      uint8_t* d = ptr_of_lane(dst, e);
+      const int slot = __shfl(ds, e, 64);
+      if (live) *(uint2*)(d + kvq_key_at(slot, lane % KL * 8)) = kr[j];
+    }
+    {
+      const bool live = ptr_of_lane(src, lane / 2) != nullptr;
+      uint8_t* d = ptr_of_lane(dst, lane / 2);
+      const int slot = __shfl(ds, lane / 2, 64);
+      if (live) *(float*)(d + (lane & 1 ? kvq_value_scale_at(HD, slot) : kvq_key_scale_at(HD, slot))) = sc;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      uint8_t* d = ptr_of_lane(dst, CH + k);
+      const int slot = __shfl(ds, CH + k, 64);
+      const unsigned on = group(mask, k);
+      if (lane < VL && on) {
+        u32x4 w = old[k];
+        const unsigned x0 = group(got[0], k), x1 = group(got[1], k);
+        if (slot & 16) {
+          w.y = (w.y & ~on) | (x0 & on);
+          w.w = (w.w & ~on) | (x1 & on);
+        } else {
+          w.x = (w.x & ~on) | (x0 & on);
+          w.z = (w.z & ~on) | (x1 & on);
+        }
+        *(u32x4*)(d + values_at(slot)) = w;
+      }
     }
   }
 }
