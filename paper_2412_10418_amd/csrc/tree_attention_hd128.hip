@@ -35,17 +35,25 @@ TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, i
   p.row_groups = (tiles + most_tiles - 1) / most_tiles;
   p.wg_tiles = (tiles + p.row_groups - 1) / p.row_groups;
   // Keys are split until there are two workgroups a CU (few rows, tiles of 32) or
-  // three, in parts of eight pages (few rows: two a wave) or four at least.  More and
-  // smaller parts start more often than they balance (at 512, 768 and 1024
+  // three.  More parts start more often than they balance (at 512, 768 and 1024
   // workgroups: 32 prompts of one token at 4096: 38, 38, 42 us; 8 trees of 65 at
   // 8192: 248, 151, 153; 4 of 40 at 4000: 34.6, 32.7, 38.8).  Less than two
   // parts a prompt only where prompts are long and 1.5 are to be had (12 trees
-  // of 65: at 8192 198 us instead of 252, at 2048 72 either way; 16 of 51 at 256:
-  // 45 instead of 28).  Few rows over a long cache are split in two whatever
+  // of 65: at 8192 198 us instead of 252, at 2048 72 either way).
+  //
+  // A part has 16 pages or more (few rows: four a wave), or 4 and one more for
+  // every 1024 rows of 128, since those are written, read and merged per part (at
+  // 256 and 1024 tokens, 8 trees of 51 x 32 heads take 20 and 42 us whole, 32
+  // and 46 in parts of 4; one tree 16.7 and 20 in parts of 4, 28 at 1024 in parts of
+  // 16).  Few rows: not below 48 pages (one token at 512: 11 us whole, 16.5 in
+  // parts of 8; at 1024 13.6 and 14.8 in two; at 2048 21 and 14.8 in four), nor
+  // below 128 where a workgroup a CU starts anyway (8 prompts x 32 KV heads at
+  // 2048: 27 whole, 31.5).  Few rows over a long cache are split in two whatever
   // their number: one prompt of 16384 among 63 short ones takes 37 us instead of
   // 116, 64 of up to 8192 115 instead of 119.
-  p.split_pages = p.few ? 8 : 4;
-  const long long most = std::min<long long>(std::max<long long>(1, pages / p.split_pages), kTreeMaxSplits);
+  p.split_pages = p.few ? 16 : (int)(4 + ((long long)B * n * H * hd >> 17));
+  long long most = std::min<long long>(std::max<long long>(1, pages / p.split_pages), kTreeMaxSplits);
+  if (p.few && pages < (pairs >= 256 ? 128 : 48)) most = 1;
   const bool shared = B > 1 && B <= kTreeShared;
   long long slots = p.few ? 512 / Hkv : p.wide ? 512 / (Hkv * two) : 768 / (Hkv * one);
   if (p.few && shared && pages >= 256) slots = std::max(slots, 2ll * B);
