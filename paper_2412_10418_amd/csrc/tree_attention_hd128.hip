@@ -15,11 +15,12 @@ TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, i
   const int tiles = (int)(((long long)n * (H / Hkv) + 15) / 16);
   p.few = tiles <= 2 ? tiles : 0;
   // Tiles of 32 rows, of which two workgroups fit a CU:
-  //  - where they fill their workgroups, and those the chip one and a half times
-  //    or more (64 prompts x 8 KV heads of 16 tiles of 16 at up to 2048 tokens:
-  //    119 against 127 us in bf16, 194 against 201 in fp32 over int8; of 14 tiles
-  //    75.0 against 74.7, of 17 134 against 125), or in bf16 just once (32
-  //    prompts at 4096: 188 against 215; up to 4096: 128 against 124);
+  //  - where they fill their workgroups to 15 of 16, and those the chip one and a
+  //    half times or more (64 prompts x 8 KV heads of 16 tiles of 16 at up to 2048
+  //    tokens: 119 against 127 us in bf16, 194 against 201 in fp32 over int8; of
+  //    14 tiles 75.0 against 74.7, of 17 134 against 125; chunks of 500 x 4 at 1000,
+  //    12 prompts: 191 against 207), or in bf16 just once (32 prompts at 4096: 188
+  //    against 215; up to 4096: 128 against 124);
   //  - where the keys are split anyway, are many, and half the workgroups take
   //    the rows (8 prompts of 17 x 4 rows at 8192: 62 against 68 us in bf16, 85
   //    against 90 in fp32; 32: 184 against 240 and 281 against 331; but 8 of 32 x
@@ -28,7 +29,7 @@ TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, i
   const long long pairs = (long long)B * Hkv;
   const long long one = (tiles + 3) / 4, two = (tiles + 7) / 8, full = pairs * two;
   const long long pages = ((long long)max_len + n + kPage - 1) / kPage;
-  const bool filled = 8 * two - tiles <= 1 && (full >= 768 || (dtype == 1 && full >= 448 && full <= 512));
+  const bool filled = 16 * (8 * two - tiles) <= 8 * two && (full >= 768 || (dtype == 1 && full >= 448 && full <= 512));
   const bool split = one == 2 * two && full * 3 <= 512 * 2 && pages >= 128 && full * pages >= 8192;
   p.wide = !p.few && (filled || split) && tree_may_be_wide(hd, dtype, format);
   const int most_tiles = p.few ? p.few : p.wide ? 8 : 4;
