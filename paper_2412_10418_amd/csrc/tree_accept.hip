@@ -277,11 +277,14 @@ __global__ __launch_bounds__(NT) void tree_sums_kernel(AcceptArgs a) {
   if (lane == 0) a.parts[slot * segs + blockIdx.x * NW + wv] = s;
 }
 
-// HELD: V <= kHeld * CHUNK, the one launch; else the one after the rounds.
-template <bool HELD>
+// CHUNKS: V <= CHUNKS * CHUNK, the one launch (one chunk of registers takes 18 us
+// over 16384 ids and 27 for 45 prompts over 12368, where two take 22.5 and 35);
+// 0: the one after the rounds.
+template <int CHUNKS>
 __global__ __launch_bounds__(NT) void tree_accept_kernel(AcceptArgs a) {
+  constexpr bool HELD = CHUNKS > 0;
   __shared__ Walk w;
-  __shared__ double part[HELD ? kHeld * NW : kSegs];
+  __shared__ double part[HELD ? CHUNKS * NW : kSegs];
   __shared__ int hit, best_i[NW];
   __shared__ float best_v[NW];
   const int b = blockIdx.x, V = a.V, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(AcceptArgs a) {
   }
   const float* p = a.p + (row0 + at.cur) * V;
   const float* q = a.q + (row0 + at.cur) * V;
-  Piece hp[HELD ? kHeld : 1], hq[HELD ? kHeld : 1];
+  Piece hp[HELD ? CHUNKS : 1], hq[HELD ? CHUNKS : 1];
   bool have_p = false, have_q = false;   // the held pieces are those of the node reached
 
   while (walk_on(w, nb, at, [&](int k, int place) {
@@ -315,19 +318,19 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(AcceptArgs a) {
     if constexpr (HELD) {
       const bool lp = !have_p, lq = !have_q && c > 0.;
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
+      for (int k = 0; k < CHUNKS; ++k) {
         if (lp) hp[k].load(p, CHUNK * k + at0, V);
         if (lq) hq[k].load(q, CHUNK * k + at0, V);
         else if (c == 0.) hq[k] = Piece{};
       }
       have_p = true;
       have_q = c > 0.;
-      double s[kHeld];
+      double s[CHUNKS];
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) s[k] = wave_sum_d(weights(hp[k], hq[k], c));
+      for (int k = 0; k < CHUNKS; ++k) s[k] = wave_sum_d(weights(hp[k], hq[k], c));
       if (lane == 0)
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k)
+        for (int k = 0; k < CHUNKS; ++k)
           if (k < chunks) part[k * NW + wv] = s[k];
     } else {
       // the next chunk's loads are in flight while one is added up
@@ -504,7 +507,8 @@ hipError_t tree_accept_launch(const float* p, const float* q, int B, int n, int 
   a.next_token = next_token;
   a.kid_stride = (long long)B * n;
   if (V <= kHeld * CHUNK) {
-    tree_accept_kernel<true><<<B, NT, 0, st>>>(a);
+    if (V <= CHUNK) tree_accept_kernel<1><<<B, NT, 0, st>>>(a);
+    else tree_accept_kernel<kHeld><<<B, NT, 0, st>>>(a);
     return hipGetLastError();
   }
   const AcceptWs ws = accept_ws(B, n, V);
@@ -518,7 +522,7 @@ hipError_t tree_accept_launch(const float* p, const float* q, int B, int n, int 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  tree_accept_kernel<false><<<B, NT, 0, st>>>(a);
+  tree_accept_kernel<0><<<B, NT, 0, st>>>(a);
   return hipGetLastError();
 }
 
