@@ -23,7 +23,7 @@
 // fp64 rate of one CU (3 us for a sum over 32000 ids, 13 us over 128256).  Rows
 // of up to 32768 ids: one workgroup per prompt, which keeps a node's rows in
 // its registers for the node's further sums and the draw.  Longer rows: the
-// first kRounds sums have a launch each, with a workgroup per chunk of the
+// first sums (rounds_of) have a launch each, with a workgroup per chunk of the
 // row; each of them walks to the next sum that is needed, from where the
 // launch before stopped, and a last launch, one workgroup per prompt, adds up
 // what is left and draws.
@@ -39,7 +39,7 @@ constexpr int RUN = 1024;                       // consecutive ids of a wave in 
 constexpr int CHUNK = NW * RUN;
 constexpr int kSegs = kAcceptMaxVocab / RUN;    // (chunk, wave) sums at most
 constexpr int kHeld = 2;                        // chunks that registers hold
-constexpr int kRounds = 4;                      // sums of a long row that have a launch of their own
+constexpr int kRounds = 5;                      // sums of a long row that have a launch of their own, at most
 
 // Sum over a wave, the same bits in every lane: rotations within rows of 16,
 // then swaps of rows and halves (a shuffle through LDS takes five times as long).
@@ -468,6 +468,12 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(AcceptArgs a) {
 
 int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
 
+// The more prompts, the longer the longest walk; the longer the rows, the more a
+// sum in the last launch costs.  With 2, 4 and 5 rounds: 8 trees over 65536 take
+// 21.6, 25.4 and 27.9 us, 8 over 128256 40.6, 31.2 and 33.6, 32 over 128256 71,
+// 55 and 50.
+int rounds_of(int B, int V) { return B >= 32 ? kRounds : B <= 16 && V <= 4 * CHUNK ? 2 : 4; }
+
 }  // namespace
 
 namespace {
@@ -516,7 +522,8 @@ hipError_t tree_accept_launch(const float* p, const float* q, int B, int n, int 
   a.parts = (double*)((char*)workspace + ws.parts);
   a.kids = (float*)((char*)workspace + ws.kids);
   const dim3 grid((unsigned)chunks_of(V), (unsigned)B);
-  for (; a.round < kRounds; ++a.round) {
+  const int rounds = rounds_of(B, V);
+  for (; a.round < rounds; ++a.round) {
     if (a.round == 0) tree_sums_kernel<true><<<grid, NT, 0, st>>>(a);
     else tree_sums_kernel<false><<<grid, NT, 0, st>>>(a);
     const hipError_t e = hipGetLastError();
