@@ -299,6 +299,27 @@ def test_batches_that_fill_the_chip(fmt, kind, hd, n, causal):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_chunks_that_fill_the_chip(kind, causal):
+    """Several row groups a prompt, the last one part empty, and prompts whose nodes end in any of them."""
+    from paper_2412_10418_amd import binding as bd
+    rng = np.random.default_rng([61, int(causal)])
+    B, n, H, heads, hd = 25, 62, 64, 8, 32
+    lens = rng.integers(0, 200, B).tolist()
+    nodes = rng.integers(0, n + 1, B)
+    nodes[[0, 7]] = n, 1
+    cache, k, v = _filled(rng, B, lens, n, heads, hd, "int8")
+    q = _rows(rng, (B, n, H, hd), "f32").to(KIND[kind])
+    parents = None if causal else np.stack([random_tree(rng, n, 3) for _ in range(B)])
+    out = torch.full_like(q, 7.0)
+    bd.cdsl_op_tree_attention(cache, q, _ints(lens), None if causal else _ints(parents), n_nodes=_ints(nodes),
+                              max_len=200, out=out)
+    _check(out, q, k, v, lens, parents, nodes.tolist(), hd ** -0.5, kind)
+    for b in range(B):
+        assert bool((out[b, nodes[b]:] == 7).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("L", [3, 2500])
 def test_nodes_that_a_prompt_lacks(kind, L):
     """Fewer nodes than n, none, and counts out of range: the rows behind are left as they were."""
@@ -523,6 +544,23 @@ def test_many_siblings_are_rejected(replace, V):
     u = np.full((B, n), 0.999, np.float32)
     _, m, _ = _verify(p, q, tokens, parents, u, rng.random(B, np.float32), replace)
     assert min(m) == 1
+
+
+@pytest.mark.parametrize("replace", [True, False])
+@pytest.mark.parametrize("B,V", [(33, 33001), (17, 40000), (16, 70000)])
+def test_batches_of_long_rows(replace, B, V):
+    """Walks of unlike lengths in one batch: prompts that are over in the first launch, others that reject seven
+    siblings and go on from the eighth."""
+    rng = np.random.default_rng([B, V])
+    n = 10
+    z = rng.standard_normal((B, n, V), np.float32)
+    p, q = _soft(z + 2 * (rng.random((B, 1, 1)) < 0.5) * rng.standard_normal((B, n, V), np.float32)), _soft(z)
+    parents = np.tile(np.array([-1] + [0] * 8 + [8], np.int32), (B, 1))
+    tokens = np.argsort(-q[:, 0], -1)[:, :n].astype(np.int32)
+    u = np.where(rng.random((B, n)) < 0.3, 0.2, 0.999).astype(np.float32)
+    u[::3, 1:8], u[::3, 8] = 0.9999, 0.0
+    _, m, _ = _verify(p, q, tokens, parents, u, rng.random(B, np.float32), replace)
+    print(f"paths of {sorted(set(m))} nodes", flush=True)
 
 
 @pytest.mark.parametrize("V", [70, 33001])
