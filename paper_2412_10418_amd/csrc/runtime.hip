@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <mutex>
 #include <new>
@@ -2000,7 +2001,7 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, 
     a.n = n;
     a.H = H;
     a.G = H / cache->n_kv_heads;
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_log2 = std::min(std::max(scale * 1.4426950408889634f, -FLT_MAX), FLT_MAX);
     return launched(tree_attn_launch(a, p, dtype, workspace, (hipStream_t)stream));
   });
 }

@@ -292,19 +292,24 @@ __device__ __forceinline__ void load_q8(const QT* p, float (&x)[8]) {
   }
 }
 
-// The power of two that brings a row of q to a largest entry in [1, 2), from
+// The power of two 2^-e that brings a row of q to a largest entry in [1, 2), from
 // the largest bit pattern of |q|: what the entries are multiplied by (with the
 // sign of the softmax scale; 0 for a scale of 0), and what a score of the
-// result counts in log2 units.  Rows of zeros and of the smallest numbers
-// count as 2^-126; a NaN or an infinity stays one (its scores are NaN).
+// result counts in log2 units, |scale| 2^e.  That factor meets the -inf of hidden
+// slots and scores of 0, so it stays finite and above 0: e is at least what
+// makes it 2^-126 (the row then keeps fewer bits, of scores below 2^-49 for keys
+// of up to 2^60), and it ends at the largest fp32.  A NaN or an infinity stays
+// one (its scores are NaN).
 struct QScale {
   float down, rm;
 };
 __device__ __forceinline__ QScale q_scale(float scale_log2, unsigned top) {
-  const int e = max((int)(top >> 23), 1) - 127;
+  const float s = fabsf(scale_log2);
+  // s >= 2^(x - 1), x the exponent of frexp
+  const int e = max(max((int)(top >> 23), 1) - 127, -125 - __builtin_amdgcn_frexp_expf(s));
   // (2^-127 and 2^-128 are subnormal, which products keep)
   return {__builtin_ldexpf(scale_log2 < 0.f ? -1.f : scale_log2 > 0.f ? 1.f : 0.f, -e),
-          scale_log2 == 0.f ? 1.f : __builtin_ldexpf(fabsf(scale_log2), e)};
+          s == 0.f ? 1.f : fminf(__builtin_ldexpf(s, e), 3.4028234663852886e38f)};
 }
 template <int QP>
 __device__ __forceinline__ void q_planes(const float (&x)[8], float down, f16x8 (&q)[QP]) {
