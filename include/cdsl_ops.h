@@ -197,7 +197,9 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V,
  * Query head h reads KV head h / (H / n_kv_heads).  scale multiplies q . k
  * before the softmax.  Rows of nodes from n_nodes[b] on are left as they
  * were.  Products, sums and softmax statistics are those of fp32, but for the
- * probabilities of a bf16 call, which are rounded to bf16.  A prompt whose
+ * probabilities of a bf16 call, which are rounded to bf16, and for entries of Q
+ * below 2^-15 (bf16: 2^-31) of their row's largest, which are off by up to 2^-39
+ * of that.  A prompt whose
  * lens[b] + n_nodes[b] its table cannot hold gets NaN rows.
  * max_len: a bound on lens, known to the host; it only decides how the keys
  * are split over the chip (0: not known, as for short prompts).  The

@@ -15,8 +15,10 @@
 //   O^T[16 dims, 16 rows] += V^T[16 dims, 32 keys] . P^T[32 keys, 16 rows].
 //
 // Precision.  A row of q is scaled by a power of two to a largest entry in
-// [1, 2) and taken as f16 planes: two for fp32 activations (24 bits of the
-// largest entry), one for bf16 (exact down to 2^-17 of the largest entry).
+// [2^14, 2^15), the top of f16, and taken as f16 planes: two for fp32 activations
+// (each entry to 2^-24 of itself or 2^-39 of the largest, whichever is more), one
+// for bf16 (exact down to 2^-31 of the largest).  The key codes are taken times
+// 2^-14 in turn, exact in f16, whose subnormals the products keep.
 // Probabilities times s_v can be of any size, so they stay bf16: three planes
 // (their 24 bits) for fp32, one (2^-8 of each, independent over the keys; the
 // result rounds by as much) for bf16.  Two planes would lose 2^-16 of each
@@ -73,7 +75,7 @@ __device__ __forceinline__ bf16x8 codes_bf16(unsigned a, unsigned b) {
   return o.v;
 }
 
-// Eight codes as f16, exact.
+// Eight key codes times 2^-14 as f16, exact (e4m3: down to 2^-23, a subnormal).
 template <int FMT>
 __device__ __forceinline__ f16x8 codes_f16(unsigned a, unsigned b) {
   union {
@@ -82,20 +84,21 @@ __device__ __forceinline__ f16x8 codes_f16(unsigned a, unsigned b) {
     f16x8 v;
   } o;
   if constexpr (FMT == kE4M3) {
-    o.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false);
-    o.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
-    o.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false);
-    o.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
+    o.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 0x1p-14f, false);
+    o.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 0x1p-14f, true);
+    o.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 0x1p-14f, false);
+    o.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 0x1p-14f, true);
   } else {
-    // 0x6400 + x is 1024 + x in f16: with x = code + 128, one subtraction
-    const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+    // 0x6400 + x is 1024 + x in f16: with x = code + 128, one multiply-add
+    const f16x2 down = {(_Float16)0x1p-14f, (_Float16)0x1p-14f};
+    const f16x2 off = {(_Float16)(-1152 * 0x1p-14f), (_Float16)(-1152 * 0x1p-14f)};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const unsigned w = (i ? b : a) ^ 0x80808080u;
       o.u[2 * i] = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400);
       o.u[2 * i + 1] = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402);
-      o.p[2 * i] -= off;
-      o.p[2 * i + 1] -= off;
+      o.p[2 * i] = __builtin_elementwise_fma(o.p[2 * i], down, off);
+      o.p[2 * i + 1] = __builtin_elementwise_fma(o.p[2 * i + 1], down, off);
     }
   }
   return o.v;
@@ -292,23 +295,23 @@ __device__ __forceinline__ void load_q8(const QT* p, float (&x)[8]) {
   }
 }
 
-// The power of two 2^-e that brings a row of q to a largest entry in [1, 2), from
-// the largest bit pattern of |q|: what the entries are multiplied by (with the
-// sign of the softmax scale; 0 for a scale of 0), and what a score of the
-// result counts in log2 units, |scale| 2^e.  That factor meets the -inf of hidden
-// slots and scores of 0, so it stays finite and above 0: e is at least what
-// makes it 2^-126 (the row then keeps fewer bits, of scores below 2^-49 for keys
-// of up to 2^60), and it ends at the largest fp32.  A NaN or an infinity stays
-// one (its scores are NaN).
+// The power of two 2^(14 - e) that brings a row of q to a largest entry in [2^14,
+// 2^15), from the largest bit pattern of |q|: what the entries are multiplied by
+// (with the sign of the softmax scale; 0 for a scale of 0), and what a score of
+// the result (with key codes of 2^-14) counts in log2 units, |scale| 2^e.  The
+// former is finite from e = -112 on.  The latter meets the -inf of hidden slots
+// and scores of 0, so it stays finite and above 0: e is at least what makes it
+// 2^-126, and it ends at the largest fp32.  (A row that e is too large for keeps
+// fewer bits, those of entries below 2^-137 or of scores below 2^-49 for keys of
+// up to 2^60 among them.)  A NaN or an infinity stays one (its scores are NaN).
 struct QScale {
   float down, rm;
 };
 __device__ __forceinline__ QScale q_scale(float scale_log2, unsigned top) {
   const float s = fabsf(scale_log2);
   // s >= 2^(x - 1), x the exponent of frexp
-  const int e = max(max((int)(top >> 23), 1) - 127, -125 - __builtin_amdgcn_frexp_expf(s));
-  // (2^-127 and 2^-128 are subnormal, which products keep)
-  return {__builtin_ldexpf(scale_log2 < 0.f ? -1.f : scale_log2 > 0.f ? 1.f : 0.f, -e),
+  const int e = max(max((int)(top >> 23) - 127, -112), -125 - __builtin_amdgcn_frexp_expf(s));
+  return {__builtin_ldexpf(scale_log2 < 0.f ? -1.f : scale_log2 > 0.f ? 1.f : 0.f, 14 - e),
           s == 0.f ? 1.f : fminf(__builtin_ldexpf(s, e), 3.4028234663852886e38f)};
 }
 template <int QP>

@@ -4,19 +4,22 @@ import pytest
 import torch
 
 from test_gpu_tree_ops import KIND, _check, _ints, _np, _rows
-from tree_cases import WHOLE, params
-from tree_ref import paged, random_tree
+from tree_cases import ALL, WHOLE, params, rms
+from tree_ref import attention, paged, random_tree
 
 pytestmark = pytest.mark.gpu
 
 
-def _filled(rng, case, fmt):
-    """The case's cache, the prompt lengths, and the keys and values of its first and last prompt in float64."""
+def _filled(rng, case, fmt, quiet=None):
+    """The case's cache, the prompt lengths, and the keys and values of its first and last prompt in float64.  quiet: a
+    channel in which all keys are 0."""
     from paper_2412_10418_amd import binding as bd
     lens = case.lens(rng)
     T = max(lens) + case.n
     cache = paged(rng, 1, case.B, T, case.heads, case.hd, fmt)
     K, V = (_rows(rng, (case.B, T, case.heads, case.hd), "f32") for _ in range(2))
+    if quiet is not None:
+        K[..., quiet] = 0
     count = _ints([l + case.n for l in lens])
     bd.cdsl_op_kvq_write(cache, K, V, count=count)
     k, v = bd.cdsl_op_kvq_read(cache, T, count=count)
@@ -45,3 +48,36 @@ def test_queries_and_scales_of_any_size(case, kind, fmt, scale):
     _check(out[some], q[some], k, v, [lens[b] for b in some], parents[some], [case.n] * len(some), scale,
            f"{case.name} {kind} {fmt} {scale}")
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("outlier", [0, 1e3, 1e5])
+@pytest.mark.parametrize("case,kind,fmt", params(ALL))
+def test_results_are_as_near_as_their_products(case, kind, fmt, outlier):
+    """With `outlier`, every row of q has an entry of that size (bf16: 2^20) in a channel in which the keys are 0: what a
+    scaled row loses of its other entries is then all the error there is.
+
+    fp32: a score (size s, 1.4 here) is a sum of 2 x 128 products, each addition off by at most 2^-24 s and by 0.3 of
+    that in the mean square: 16 x 0.3 x 1.4 x 2^-24 = 4e-7 of a probability; its exponential and the sums over the keys
+    as much again: 1e-6 in all.  (Probabilities of 16 bits, 2^-16 at most, would give 2.5e-6; entries of q to 2^-25 of an
+    outlier of 1e3 3e-5.)  bf16: beside the results' own rounding each probability is rounded, by itself and by half
+    a step, 2^-8 of it, at most, so in a sum of independent terms the mean square grows by 2^-16 of the results' at most."""
+    from paper_2412_10418_amd import binding as bd
+    rng = np.random.default_rng([case.B, case.n, 72])
+    cache, lens, some, k, v = _filled(rng, case, fmt, quiet=5)
+    q = 0.5 * torch.from_numpy(rng.standard_normal((case.B, case.n, case.H, case.hd), np.float32)).cuda()
+    if outlier:
+        size = outlier if kind == "f32" else 2.0 ** 20
+        q[..., 5] = size * torch.from_numpy(rng.choice(np.float32([-1.7, -1, 1, 1.3]), q.shape[:3])).cuda()
+    q = q.to(KIND[kind])
+    parents = np.stack([random_tree(rng, case.n, 3) for _ in range(case.B)])
+    out = _np(bd.cdsl_op_tree_attention(cache, q, _ints(lens), _ints(parents), max_len=case.longest))
+    off, own, ref = [], [], []
+    for i, b in enumerate(some):
+        o, _, _ = attention(_np(q[b]).astype(np.float64), k[i][:lens[b] + case.n], v[i][:lens[b] + case.n], lens[b],
+                            parents[b], case.hd ** -0.5)
+        off.append((out[b] - o).ravel())
+        own.append((_np(torch.from_numpy(o).to(KIND[kind])) - o).ravel())
+        ref.append(o.ravel())
+    off, own, ref = (rms(np.concatenate(x)) for x in (off, own, ref))
+    print(f"{case.name} {kind} {fmt}: off by {off / ref:.3g} of the results, their own rounding {own / ref:.3g}", flush=True)
+    assert off <= 1e-6 * ref if kind == "f32" else off ** 2 <= own ** 2 + (2.0 ** -8 * ref) ** 2

@@ -3,6 +3,8 @@ that the plan takes for a row type and a cache format.
 
 few1, few2: one or two tiles of 16 rows a workgroup; many3, many4: pages staged for four waves, three or four of them a
 SIMD; wide: tiles of 32 rows; +split: the keys of a prompt over several workgroups."""
+import numpy as np
+
 KINDS, FMTS = ("f32", "bf16"), ("int8", "e4m3")
 
 
@@ -58,3 +60,7 @@ def params(cases=None):
     import pytest
     return [pytest.param(c, k, f, id=f"{c.name}-{k}-{f}".replace(" ", "_")) for c in cases or ALL for k in KINDS for f in FMTS]
 
+
+
+def rms(x):
+    return float(np.sqrt(np.mean(np.square(np.asarray(x, np.float64)))))
