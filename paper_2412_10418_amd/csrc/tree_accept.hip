@@ -87,21 +87,29 @@ __device__ __forceinline__ double weight(float p, float q, double c) {
   const double d = fma(-c, (double)q, (double)p);
   return d < 0. ? 0. : d;
 }
-// Their sum as half of sum d + sum |d|: a subtraction and two additions an
-// entry, and a NaN stays one (the fp64 instructions bound a pass: a maximum
-// that keeps NaNs takes three).  Without an entry above 0 the two cancel to
-// exactly 0, since every partial sum has its negative.
+// Their sum: three fp64 instructions an entry behind the conversions (they bound
+// a pass).  A maximum drops NaNs, so they are looked for among the entries where
+// one is 2 or above, which no probability is.  Each term is taken at 0 before it
+// is added: sum d and sum |d|, whose half it is as well, lose what is left
+// beside rejected tokens once c is large.
 __device__ __forceinline__ double weights(const Piece& p, const Piece& q, double c) {
-  double d = 0., a = 0.;
+  double s = 0.;
+  unsigned bits = 0;
 #pragma unroll
   for (int u = 0; u < 4; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const double t = fma(-c, (double)q.x[u][e], (double)p.x[u][e]);
-      d += t;
-      a += fabs(t);
+      s += fmax(fma(-c, (double)q.x[u][e], (double)p.x[u][e]), 0.);
+      bits |= __float_as_uint(p.x[u][e]) | __float_as_uint(q.x[u][e]);
     }
-  return 0.5 * (d + a);
+  if (bits & 0x40000000u) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (__builtin_isunordered(p.x[u][e], q.x[u][e])) s = NAN;
+  }
+  return s;
 }
 
 struct AcceptArgs {

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_tree_ops import KIND, _check, _ints, _np, _rows
+from test_gpu_tree_ops import KIND, _check, _ints, _np, _rows, _verify
 from tree_cases import ALL, WHOLE, params, rms
 from tree_ref import attention, paged, random_tree
 
@@ -81,3 +81,30 @@ def test_results_are_as_near_as_their_products(case, kind, fmt, outlier):
     off, own, ref = (rms(np.concatenate(x)) for x in (off, own, ref))
     print(f"{case.name} {kind} {fmt}: off by {off / ref:.3g} of the results, their own rounding {own / ref:.3g}", flush=True)
     assert off <= 1e-6 * ref if kind == "f32" else off ** 2 <= own ** 2 + (2.0 ** -8 * ref) ** 2
+
+
+@pytest.mark.parametrize("V", [3001, 32768, 40001])
+@pytest.mark.parametrize("v", [0.6995 / 0.9, 0.7005 / 0.9, 0.3995 / 0.9, 0.4005 / 0.9])
+def test_what_is_left_of_a_draft_that_is_nearly_used_up(V, v):
+    """Three siblings drawn without replacement leave 2^-45 of the draft, so that the rejected tokens' terms are 2^45 times
+    what the target has left beside them; the draws are 5e-4 from a border."""
+    p, q = np.zeros((1, 4, V), np.float32), np.zeros((1, 4, V), np.float32)
+    for t, x in ((11, 0.4), (200, 0.1), (400, 0.3), (500, 0.2)):
+        p[:, :, t] = x
+    for t, x in ((10, 1 - 2.0 ** -24), (200, 2.0 ** -24 - 2.0 ** -45), (300, 2.0 ** -46)):
+        q[:, :, t] = x
+    tokens, parents = np.array([[0, 10, 200, 300]], np.int32), np.array([[-1, 0, 0, 0]], np.int32)
+    _verify(p, q, tokens, parents, np.full((1, 4), 0.9, np.float32), np.full(1, v, np.float32), False)
+
+
+@pytest.mark.parametrize("V", [300, 20000, 40001])
+@pytest.mark.parametrize("at", [0, 17, 299])
+@pytest.mark.parametrize("bad", [np.nan, -np.nan])
+def test_a_nan_in_the_draft_row_of_a_rejection(V, at, bad):
+    """It is in the sum of what is left: no token."""
+    from paper_2412_10418_amd import binding as bd
+    p, q = np.full((1, 2, V), 1 / V, np.float32), np.full((1, 2, V), 1 / (2 * V), np.float32)
+    q[:, :, 5], q[0, 0, at] = 1, bad
+    f = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda()  # noqa: E731
+    path, m, tok = bd.cdsl_op_tree_accept(f(p), f(q), _ints([[0, 5]]), _ints([[-1, 0]]), f([[0.9, 0.9]]), f([0.5]))
+    assert path.tolist() == [[0, -1]] and m.tolist() == [1] and tok.tolist() == [-1]
