@@ -204,7 +204,8 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V,
  * max_len: a bound on lens, known to the host; it only decides how the keys
  * are split over the chip (0: not known, as for short prompts).  The
  * workspace must hold cdsl_op_tree_attention_workspace bytes for the same
- * arguments (0: none needed); it needs no initial contents.  Results do not
+ * arguments (0: none needed, or arguments that the call refuses); it needs no
+ * initial contents.  Results do not
  * depend on other calls, and the same arguments give the same bits.  Errors:
  * EINVAL, ERANGE (n beyond CDSL_TREE_MAX with parents, batch * n * H of 2^24
  * or more), EDEVICE. */

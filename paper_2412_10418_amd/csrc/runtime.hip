@@ -1921,6 +1921,11 @@ int kvq_rows_check(const cdsl_kvq* c, int32_t layer, const void* K, const void* 
   return CDSL_OK;
 }
 
+// rows of a tree attention that a launch, and the plan's arithmetic, can take
+bool tree_rows_fit(int32_t batch, int32_t n, int32_t H) {
+  return batch <= 65535 && (long long)n * H <= kMaxGroups && batch * ((long long)n * H) <= kMaxGroups;
+}
+
 int launched(hipError_t e) {
   return e == hipSuccess ? CDSL_OK : fail(nullptr, CDSL_EDEVICE, hipGetErrorString(e));
 }
@@ -1959,7 +1964,9 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V, int
 
 size_t cdsl_op_tree_attention_workspace(int32_t batch, int32_t n, int32_t H, int32_t n_kv_heads, int32_t head_dim,
                                         int32_t max_len) {
-  if (batch <= 0 || n <= 0 || H <= 0 || n_kv_heads <= 0 || H % n_kv_heads != 0 || (long long)n * H > (1 << 30)) return 0;
+  if (batch <= 0 || n <= 0 || H <= 0 || n_kv_heads <= 0 || H % n_kv_heads != 0) return 0;
+  if (head_dim != 32 && head_dim != 64 && head_dim != 128) return 0;
+  if (!tree_rows_fit(batch, n, H)) return 0;
   return tree_attn_workspace(batch, n, H, n_kv_heads, head_dim, std::max(max_len, 0));
 }
 
@@ -1980,12 +1987,12 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, 
     if (!aligned_stride(q_stride_b, dtype) || !aligned_stride(q_stride_t, dtype))
       return fail(nullptr, CDSL_EINVAL, "row strides must be multiples of 16 bytes");
     if (parents && n > CDSL_TREE_MAX) return fail(nullptr, CDSL_ERANGE, "a tree has at most 512 nodes");
-    if ((long long)n * H > (1 << 30)) return fail(nullptr, CDSL_ERANGE, "n * H exceeds 2^30");
     if (cache->batch == 0 || n == 0) return CDSL_OK;
+    // before the plan, whose arithmetic holds for these sizes
+    if (!tree_rows_fit(cache->batch, n, H)) return fail(nullptr, CDSL_ERANGE, "too many rows");
     const TreeAttnPlan p = tree_attn_plan(cache->batch, n, H, cache->n_kv_heads, cache->head_dim, std::max(max_len, 0),
                                           dtype, cache->format);
-    if ((long long)p.row_groups * p.slots * cache->n_kv_heads > kMaxGroups ||
-        (long long)cache->batch * n * H > kMaxGroups)
+    if ((long long)p.row_groups * p.slots * cache->n_kv_heads > kMaxGroups)
       return fail(nullptr, CDSL_ERANGE, "too many rows");
     if (p.workspace > 0 && (!workspace || workspace_bytes < p.workspace))
       return fail(nullptr, CDSL_EINVAL, "workspace too small");

@@ -1,0 +1,20 @@
+"""Sizes at the ends of their types in the calls around a drafted tree: refused on the host, without a GPU."""
+import pytest
+
+from test_tree_ops_host import _attend, _cache
+
+
+def test_rows_beyond_the_launch_are_refused_before_they_are_planned():
+    """Sizes whose products pass 32 and 64 bits: the plan divided by what was left of one."""
+    from paper_2412_10418_amd import binding as bd
+    c = _cache(batch=4096, n_kv_heads=1, head_dim=128)
+    assert _attend(c, n=2 ** 30 - 1, H=1) == bd.CDSL_ERANGE
+    assert _attend(_cache(batch=65535, n_kv_heads=1), n=2 ** 31 - 1, H=2 ** 31 - 1) == bd.CDSL_ERANGE
+
+
+@pytest.mark.parametrize("args", [(2 ** 30 - 1, 4096, 1, 1, 128, 30000), (4096, 2 ** 30 - 1, 1, 1, 128, 0),
+                                  (2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 1, 128, 2 ** 31 - 1), (65536, 1, 1, 1, 64, 5000),
+                                  (1, 2 ** 24, 1, 1, 64, 5000), (1, 1, 8, 8, 48, 30000)])
+def test_no_workspace_for_what_is_refused(args):
+    from paper_2412_10418_amd import binding as bd
+    assert bd.lib().cdsl_op_tree_attention_workspace(*args) == 0
