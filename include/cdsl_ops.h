@@ -160,7 +160,7 @@ typedef struct cdsl_kvq {
 
 /* Bytes of the pool: n_layers * pages * n_kv_heads units of
  * 64 * head_dim + 256 bytes, laid out [layer][page][head].  0 for arguments
- * out of range. */
+ * out of range and pools of 2^62 bytes or more. */
 size_t cdsl_op_kvq_pool_bytes(int32_t n_layers, int32_t pages,
                               int32_t n_kv_heads, int32_t head_dim);
 

@@ -1897,6 +1897,8 @@ int kvq_check(const cdsl_kvq* c) {
   if (c->format != CDSL_KVQ_INT8 && c->format != CDSL_KVQ_E4M3) return fail(nullptr, CDSL_EINVAL, "bad cache format");
   if (!aligned16(c->pool)) return fail(nullptr, CDSL_EINVAL, "the pool must be 16-byte aligned");
   if (c->batch > 65535) return fail(nullptr, CDSL_ERANGE, "more than 65535 prompts");
+  if (cdsl_op_kvq_pool_bytes(c->n_layers, c->pages, c->n_kv_heads, c->head_dim) == 0)
+    return fail(nullptr, CDSL_ERANGE, "pool beyond 2^62 bytes");
   return CDSL_OK;
 }
 
@@ -1936,7 +1938,8 @@ extern "C" {
 
 size_t cdsl_op_kvq_pool_bytes(int32_t n_layers, int32_t pages, int32_t n_kv_heads, int32_t head_dim) {
   if (n_layers <= 0 || pages <= 0 || n_kv_heads <= 0 || (head_dim != 32 && head_dim != 64 && head_dim != 128)) return 0;
-  return (size_t)n_layers * pages * n_kv_heads * kvq_unit_bytes(head_dim);
+  const unsigned __int128 bytes = (unsigned __int128)n_layers * pages * n_kv_heads * kvq_unit_bytes(head_dim);
+  return bytes >> 62 ? 0 : (size_t)bytes;
 }
 
 int cdsl_op_kvq_write(const cdsl_kvq* cache, int32_t layer, const void* K, const void* V, int32_t dtype, int32_t T,

@@ -1,7 +1,7 @@
 """Sizes at the ends of their types in the calls around a drafted tree: refused on the host, without a GPU."""
 import pytest
 
-from test_tree_ops_host import _attend, _cache
+from test_tree_ops_host import _attend, _cache, _keep, _read, _write
 
 
 def test_rows_beyond_the_launch_are_refused_before_they_are_planned():
@@ -18,3 +18,13 @@ def test_rows_beyond_the_launch_are_refused_before_they_are_planned():
 def test_no_workspace_for_what_is_refused(args):
     from paper_2412_10418_amd import binding as bd
     assert bd.lib().cdsl_op_tree_attention_workspace(*args) == 0
+
+
+def test_pools_beyond_64_bits_have_no_size():
+    """Their bytes came out modulo 2^64: 16896 for the first."""
+    from paper_2412_10418_amd import binding as bd
+    for layers, pages, heads in ((45078, 48912491, 32681), (1 << 20, 1 << 30, 1 << 6), (2 ** 31 - 1,) * 3):
+        assert bd.lib().cdsl_op_kvq_pool_bytes(layers, pages, heads, 128) == 0
+        c = _cache(n_layers=layers, pages=pages, n_kv_heads=heads, head_dim=128)
+        assert _write(c) == _read(c) == _keep(c) == _attend(c, H=heads) == bd.CDSL_ERANGE
+    assert bd.lib().cdsl_op_kvq_pool_bytes(1 << 10, 1 << 24, 1 << 10, 128) == 8448 << 44
