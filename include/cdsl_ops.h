@@ -154,7 +154,7 @@ typedef struct cdsl_kvq {
   int32_t n_kv_heads;
   int32_t head_dim;      /* 32, 64 or 128 */
   int32_t batch;         /* prompts (<= 65535) */
-  int32_t table_stride;  /* pages per prompt */
+  int32_t table_stride;  /* pages per prompt (< 2^26) */
   int32_t format;        /* CDSL_KVQ_INT8 or CDSL_KVQ_E4M3 */
 } cdsl_kvq;
 

@@ -1897,6 +1897,8 @@ int kvq_check(const cdsl_kvq* c) {
   if (c->format != CDSL_KVQ_INT8 && c->format != CDSL_KVQ_E4M3) return fail(nullptr, CDSL_EINVAL, "bad cache format");
   if (!aligned16(c->pool)) return fail(nullptr, CDSL_EINVAL, "the pool must be 16-byte aligned");
   if (c->batch > 65535) return fail(nullptr, CDSL_ERANGE, "more than 65535 prompts");
+  // positions and the ends of their pages are ints in the kernels
+  if (c->table_stride >= (1 << 26)) return fail(nullptr, CDSL_ERANGE, "a table holds fewer than 2^26 pages a prompt");
   if (cdsl_op_kvq_pool_bytes(c->n_layers, c->pages, c->n_kv_heads, c->head_dim) == 0)
     return fail(nullptr, CDSL_ERANGE, "pool beyond 2^62 bytes");
   return CDSL_OK;

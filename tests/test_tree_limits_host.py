@@ -28,3 +28,13 @@ def test_pools_beyond_64_bits_have_no_size():
         c = _cache(n_layers=layers, pages=pages, n_kv_heads=heads, head_dim=128)
         assert _write(c) == _read(c) == _keep(c) == _attend(c, H=heads) == bd.CDSL_ERANGE
     assert bd.lib().cdsl_op_kvq_pool_bytes(1 << 10, 1 << 24, 1 << 10, 128) == 8448 << 44
+
+
+def test_tables_end_where_positions_do():
+    """The attention takes a position and the end of its page as an int: 2^26 pages of 32 tokens pass it."""
+    from paper_2412_10418_amd import binding as bd
+    for pages in (1 << 26, 2 ** 31 - 1):
+        c = _cache(table_stride=pages)
+        assert _write(c) == _read(c) == _keep(c) == _attend(c) == bd.CDSL_ERANGE
+    c = _cache(table_stride=(1 << 26) - 1)
+    assert _write(c, T=0) == _read(c, T=0) == _attend(c, n=0) == bd.CDSL_OK
