@@ -258,9 +258,9 @@ int cdsl_op_tree_accept(const float* target_probs, const float* draft_probs,
  * lens[b] + path[b][i] moves to lens[b] + i, i < n_path[b] (clamped to
  * 0..n).  path [batch][n] holds ascending nodes in [0, CDSL_TREE_MAX), as
  * cdsl_op_tree_accept writes it (or only its first n columns).  new_lens[b]
- * (NULL: not wanted; not lens itself) receives lens[b] + n_path[b].  The
- * prompts' pages from the one with position lens[b] on must be their own.
- * Errors: EINVAL, ERANGE, EDEVICE. */
+ * (NULL: not wanted; no part of lens, n_path or path) receives lens[b] +
+ * n_path[b].  The prompts' pages from the one with position lens[b] on must be
+ * their own.  Errors: EINVAL, ERANGE, EDEVICE. */
 int cdsl_op_kvq_keep(const cdsl_kvq* cache, const int32_t* lens,
                      const int32_t* path, const int32_t* n_path, int32_t n,
                      int32_t* new_lens, void* stream);

@@ -1930,6 +1930,11 @@ bool tree_rows_fit(int32_t batch, int32_t n, int32_t H) {
   return batch <= 65535 && (long long)n * H <= kMaxGroups && batch * ((long long)n * H) <= kMaxGroups;
 }
 
+// whether na ints from a on and nb from b on share any
+bool overlap(const int32_t* a, int64_t na, const int32_t* b, int64_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + 4 * nb && (uintptr_t)b < (uintptr_t)a + 4 * na;
+}
+
 int launched(hipError_t e) {
   return e == hipSuccess ? CDSL_OK : fail(nullptr, CDSL_EDEVICE, hipGetErrorString(e));
 }
@@ -2051,7 +2056,10 @@ int cdsl_op_kvq_keep(const cdsl_kvq* cache, const int32_t* lens, const int32_t* 
     if ((!lens || !n_path || (!path && n != 0)) && cache->batch != 0)
       return fail(nullptr, CDSL_EINVAL, "null argument");
     if (n < 0) return fail(nullptr, CDSL_EINVAL, "bad node count");
-    if (new_lens && new_lens == lens) return fail(nullptr, CDSL_EINVAL, "new_lens must not be lens");
+    // it is written while other workgroups still read these
+    const int64_t B = cache->batch;
+    if (new_lens && (overlap(new_lens, B, lens, B) || overlap(new_lens, B, n_path, B) || overlap(new_lens, B, path, B * n)))
+      return fail(nullptr, CDSL_EINVAL, "new_lens must not overlap lens, n_path or path");
     if ((long long)cache->n_layers * cache->n_kv_heads > kMaxGroups) return fail(nullptr, CDSL_ERANGE, "too many heads");
     return launched(kvq_keep_launch(kvq_view(cache, 0), cache->n_layers, kvq_layer_bytes(cache), lens, path, n_path, n,
                                     new_lens, (hipStream_t)stream));
