@@ -194,13 +194,14 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V,
  * n; clamped to 0..n) of prompt b sees positions [0, lens[b]), itself (at
  * lens[b] + m) and, with parents [batch][n], the nodes above it: parents[b][m]
  * in [0, m), anything else ends the way up.  parents NULL: all nodes up to m.
- * Query head h reads KV head h / (H / n_kv_heads).  scale multiplies q . k
- * before the softmax.  Rows of nodes from n_nodes[b] on are left as they
- * were.  Products, sums and softmax statistics are those of fp32, but for the
+ * A length below 0 counts as 0.  Query head h reads KV head h / (H /
+ * n_kv_heads).  scale multiplies q . k before the softmax.  Rows of nodes from
+ * n_nodes[b] on are left as they were.  A prompt whose lens[b] + n_nodes[b] its
+ * table cannot hold gets NaN rows.
+ * Products, sums and softmax statistics are those of fp32, but for the
  * probabilities of a bf16 call, which are rounded to bf16, and for entries of Q
  * below 2^-15 (bf16: 2^-31) of their row's largest, which are off by up to 2^-39
- * of that.  A prompt whose
- * lens[b] + n_nodes[b] its table cannot hold gets NaN rows.
+ * of that.
  * max_len: a bound on lens, known to the host; it only decides how the keys
  * are split over the chip (0: not known, as for short prompts).  The
  * workspace must hold cdsl_op_tree_attention_workspace bytes for the same
@@ -259,8 +260,9 @@ int cdsl_op_tree_accept(const float* target_probs, const float* draft_probs,
  * 0..n).  path [batch][n] holds ascending nodes in [0, CDSL_TREE_MAX), as
  * cdsl_op_tree_accept writes it (or only its first n columns).  new_lens[b]
  * (NULL: not wanted; no part of lens, n_path or path) receives lens[b] +
- * n_path[b].  The prompts' pages from the one with position lens[b] on must be
- * their own.  Errors: EINVAL, ERANGE, EDEVICE. */
+ * n_path[b], or 2^31 - 1 if that is more.  A length below 0 counts as 0.  The
+ * prompts' pages from the one with position lens[b] on must be their own.
+ * Errors: EINVAL, ERANGE, EDEVICE. */
 int cdsl_op_kvq_keep(const cdsl_kvq* cache, const int32_t* lens,
                      const int32_t* path, const int32_t* n_path, int32_t n,
                      int32_t* new_lens, void* stream);

@@ -324,7 +324,7 @@ __global__ __launch_bounds__(64) void kvq_keep_kernel(KvqView c, long long layer
   c.pool += layer * layer_bytes;
   const int L = max(lens[b], 0);
   const int m = min(max(n_path[b], 0), n);
-  if (new_lens && blockIdx.x == 0 && lane == 0) new_lens[b] = L + m;
+  if (new_lens && blockIdx.x == 0 && lane == 0) new_lens[b] = (int)min((long long)L + m, 0x7fffffffll);
   // a lane's 16 bytes of values in the group of four slots that holds `slot`
   auto values_at = [&](int slot) __attribute__((always_inline)) {
     const int x = lane % VL;
