@@ -201,7 +201,10 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V,
  * Products, sums and softmax statistics are those of fp32, but for the
  * probabilities of a bf16 call, which are rounded to bf16, and for entries of Q
  * below 2^-15 (bf16: 2^-31) of their row's largest, which are off by up to 2^-39
- * of that.
+ * of that.  They overflow as in fp32, before the division by the sum of the
+ * probabilities (the largest of which counts 1 to 2^8) and with rows of Q scaled
+ * to entries below 2: keys, and values times the number of keys, stay below
+ * 2^119.
  * max_len: a bound on lens, known to the host; it only decides how the keys
  * are split over the chip (0: not known, as for short prompts).  The
  * workspace must hold cdsl_op_tree_attention_workspace bytes for the same
@@ -226,8 +229,9 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q,
  * drafted tokens, tokens[b][j], under parents[b][j] in [0, j).  target_probs
  * and draft_probs [batch][n][V] (fp32, contiguous; temperature and
  * truncation are the caller's) hold in row j the target's and the draft's
- * distribution after node j; a draft row is read only where a child of its
- * node is rejected.  From the node reached (0 at first) with rows p and q,
+ * distribution after node j; both rows are read at the tokens of all their
+ * children, and whole where the walk ends (the target's) and where a child of
+ * their node is rejected.  From the node reached (0 at first) with rows p and q,
  * its children are tested in index order: child j with token x is kept when
  *   u[b][j] * q_r(x) <= P_r(x) and P_r(x) > 0
  * and becomes the node reached; otherwise P_{r+1} = max(0, P_r - q_r)
@@ -235,14 +239,15 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q,
  * draws (replace != 0), or q without the tokens rejected so far, divided by
  * what is left of 1 (replace = 0: drawn without replacement; children are
  * passed over once nothing is left).  When no child is left, next_token[b]
- * is the smallest token t with P_r(0) + ... + P_r(t) > v[b] * (sum of P_r);
- * if a rejection leaves no mass, no further child is tested and it is argmax
- * p (lowest id); -1 if p has no mass, or for a sum that is not finite.  Sums
- * and tests are in fp64.  path[b][0..n_path[b]) are the nodes reached from 0
- * on (path[b][0] = 0), the rest of path [batch][n] is -1.  n_nodes (NULL: n)
- * is clamped to 1..n.  A child whose token is outside [0, V), or whose parent
- * is outside [0, j), is passed over.  u [batch][n] and v [batch] are uniforms
- * in [0, 1).  The workspace must hold cdsl_op_tree_accept_workspace bytes (0:
+ * is the smallest token t with P_r(0) + ... + P_r(t) > v[b] * (sum of P_r), or
+ * -1 if p has no mass.  If a rejection leaves no mass, no further child is
+ * tested and next_token[b] is argmax p, the lowest id of the largest: 0 where p
+ * has no mass itself but a child was there to be rejected.  For a sum that is
+ * not finite it is -1.  Sums and tests are in fp64.  path[b][0..n_path[b]) are
+ * the nodes reached from 0 on (path[b][0] = 0), the rest of path [batch][n] is
+ * -1.  n_nodes (NULL: n) is clamped to 1..n.  A child whose token is outside
+ * [0, V), or whose parent is outside [0, j), is passed over.  u [batch][n] and
+ * v [batch] are uniforms in [0, 1).  The workspace must hold cdsl_op_tree_accept_workspace bytes (0:
  * none needed); it needs no initial contents.  Errors: EINVAL, ERANGE (batch
  * beyond 65535, n beyond CDSL_TREE_MAX, V beyond CDSL_ACCEPT_MAX_VOCAB),
  * EDEVICE. */

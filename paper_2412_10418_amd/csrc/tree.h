@@ -1,6 +1,6 @@
 // Internal interface of the 8-bit paged cache (kvq.hip), the attention of a
-// token tree over it (tree_attention.hip) and the tree's verification
-// (tree_accept.hip).
+// token tree over it (tree_attention.h, an instance file per head dimension) and
+// the tree's verification (tree_accept.hip).
 #pragma once
 #include "common.h"
 #include "kvq_layout.h"
