@@ -4,6 +4,7 @@
 #pragma once
 #include "common.h"
 #include "kvq_layout.h"
+#include "tree_plan.h"
 
 namespace cdsl {
 
@@ -23,9 +24,6 @@ hipError_t kvq_read_launch(const KvqView& c, const KvqRows& r, hipStream_t st);
 hipError_t kvq_keep_launch(const KvqView& c, int n_layers, long long layer_bytes, const int* lens, const int* path,
                            const int* n_path, int n, int* new_lens, hipStream_t st);
 
-constexpr int kTreeMaxSplits = 64;
-constexpr int kTreeShared = 64;   // prompts that share the key splits by their lengths
-
 struct TreeAttnArgs {
   KvqView c;
   const void* q;
@@ -43,18 +41,6 @@ struct TreeAttnArgs {
   int wg_tiles;            // row tiles (of 16) per workgroup
 };
 
-struct TreeAttnPlan {
-  int few;                 // 1, 2: tree_few_kernel with so many row tiles
-  bool wide;               // tree_wide_kernel; else tree_many_kernel
-  int wg_tiles;            // row tiles (of 16) per workgroup
-  int row_groups, slots, split_pages;
-  size_t workspace;
-};
-
-// fp32 over e4m3 (heads of 128) is as fast in tiles of 16 rows (188 us) as of 32 (190).
-constexpr bool tree_may_be_wide(int hd, int dtype, int format) { return !(hd == 128 && dtype == 0 && format == kE4M3); }
-TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, int dtype, int format);
-size_t tree_attn_workspace(int B, int n, int H, int Hkv, int hd, int max_len);   // enough for every type and format
 hipError_t tree_attn_launch(TreeAttnArgs a, const TreeAttnPlan& p, int dtype, void* workspace, hipStream_t st);
 
 constexpr int kAcceptMaxVocab = 1 << 20;

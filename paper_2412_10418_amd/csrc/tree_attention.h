@@ -1110,11 +1110,8 @@ hipError_t tree_attn_rows(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStrea
   if (p.few == 1) tree_few_kernel<HD, FMT, QT, 1><<<grid, 256, 0, st>>>(a);
   else if (p.few == 2) tree_few_kernel<HD, FMT, QT, 2><<<grid, 256, 0, st>>>(a);
   else if (!p.wide) {
-    // Four workgroups a CU where there are as many; fewer are faster in three (64
-    // trees of 65 at 2048 in bf16: 152 -> 146 us; 16 of them: 56 -> 61).  Heads
-    // of 64 gain nothing by it, fp32 over int8 loses 5% (231 -> 243).
-    constexpr bool kFour = HD == 128 && (sizeof(QT) == 2 || FMT == kE4M3);
-    if (kFour && grid >= 1024) tree_many_kernel<HD, FMT, QT, kFour ? 4 : 3><<<grid, 256, 0, st>>>(a);
+    constexpr bool kFour = tree_may_be_four(HD, sizeof(QT) == 2, FMT);
+    if (kFour && p.four) tree_many_kernel<HD, FMT, QT, kFour ? 4 : 3><<<grid, 256, 0, st>>>(a);
     else tree_many_kernel<HD, FMT, QT, 3><<<grid, 256, 0, st>>>(a);
   } else if constexpr (tree_may_be_wide(HD, sizeof(QT) == 2, FMT)) {
     tree_wide_kernel<HD, FMT, QT><<<grid, 256, 0, st>>>(a);

@@ -1,5 +1,5 @@
 """Shapes that reach each kernel of the tree attention: (B, n, H, KV heads, head dim, longest prompt), with the kernel
-that the plan takes for a row type and a cache format.
+that the plan takes for a row type and a cache format (test_tree_plan_host.py holds the names to it).
 
 few1, few2: one or two tiles of 16 rows a workgroup; many3, many4: pages staged for four waves, three or four of them a
 SIMD; wide: tiles of 32 rows; +split: the keys of a prompt over several workgroups."""
