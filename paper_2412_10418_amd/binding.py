@@ -322,9 +322,12 @@ def _call(dev: int, fn, *args):
 
 class QuantCache:
     """The 8-bit paged cache of a batch of prompts: pool [layers, pages, heads, unit bytes] (uint8, see
-    ``QuantCache.empty``), table [prompts, pages per prompt] (int32 page ids)."""
+    ``QuantCache.empty``), table [prompts, pages per prompt] (int32 page ids).  The calls see what is written into the
+    two tensors; for other ones make another QuantCache."""
 
-    __slots__ = ("pool", "table", "head_dim", "fmt", "batch", "n_kv_heads", "device", "_c", "_ref")
+    __slots__ = ("_pool", "_table", "_head_dim", "_fmt", "batch", "n_kv_heads", "device", "_c", "_ref")
+    pool, table = property(lambda self: self._pool), property(lambda self: self._table)
+    head_dim, fmt = property(lambda self: self._head_dim), property(lambda self: self._fmt)
 
     def __init__(self, pool: torch.Tensor, table: torch.Tensor, head_dim: int, fmt: str):
         if fmt not in _KVQ_FORMATS:
@@ -343,7 +346,7 @@ class QuantCache:
         self._c = KVQ(_of(pool, shape, torch.uint8, dev, "pool"), _of(table, table.shape, torch.int32, dev, "table"),
                       layers, pages, heads, head_dim, batch, stride, _KVQ_FORMATS[fmt])
         self._ref = C.addressof(self._c)
-        self.pool, self.table, self.head_dim, self.fmt = pool, table, head_dim, fmt
+        self._pool, self._table, self._head_dim, self._fmt = pool, table, head_dim, fmt
         self.batch, self.n_kv_heads, self.device = batch, heads, dev
 
     @staticmethod

@@ -1,4 +1,5 @@
-"""Lengths at the ends of their type in the kept path, and target rows without mass in the verification."""
+"""Lengths at the ends of their type in the kept path, target rows without mass in the verification, and caches whose
+tensors are not to be exchanged."""
 import numpy as np
 import pytest
 import torch
@@ -44,3 +45,19 @@ def test_target_rows_without_mass(V, replace):
                                           f(np.full(4, 0.5)), replace=replace)
     assert m.tolist() == [1, 1, 2, 2] and tok.tolist() == [-1, 0, -1, 0]
     assert path.tolist() == [[0, -1, -1], [0, -1, -1], [0, 1, -1], [0, 1, -1]]
+
+
+def test_a_cache_keeps_its_tensors():
+    """The library holds their addresses: another table put in the place of one had no effect on the calls."""
+    cache = paged(np.random.default_rng(82), 1, 2, 40, 2, 32, "int8")
+    for name in ("pool", "table", "head_dim", "fmt"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, getattr(cache, name))
+    # what is written into the table counts
+    from paper_2412_10418_amd import binding as bd
+    x = _rows(np.random.default_rng(83), (2, 32, 2, 32), "f32")
+    bd.cdsl_op_kvq_write(cache, x, -x)
+    k, _ = bd.cdsl_op_kvq_read(cache, 32)
+    cache.table.copy_(cache.table.flip(0))
+    k2, _ = bd.cdsl_op_kvq_read(cache, 32)
+    assert torch.equal(k2, k.flip(0))
