@@ -199,20 +199,19 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V,
  * n_nodes[b] on are left as they were.  A prompt whose lens[b] + n_nodes[b] its
  * table cannot hold gets NaN rows.
  * Products, sums and softmax statistics are those of fp32, but for the
- * probabilities of a bf16 call, which are rounded to bf16, and for entries of Q
- * below 2^-15 (bf16: 2^-31) of their row's largest, which are off by up to 2^-39
- * of that.  They overflow as in fp32, before the division by the sum of the
- * probabilities (the largest of which counts 1 to 2^8) and with rows of Q scaled
- * to entries below 2: keys, and values times the number of keys, stay below
- * 2^119.
+ * probabilities of a bf16 call, which are rounded to bf16 (to twice its bits
+ * where n * H / n_kv_heads is 16 or less), and for entries of Q below 2^-15
+ * (bf16: 2^-31) of their row's largest, which are off by up to 2^-39 of that.
+ * They overflow as in fp32, before the division by the sum of the probabilities
+ * (the largest of which counts 1 to 2^8) and with rows of Q scaled to entries
+ * below 2: keys, and values times the number of keys, stay below 2^119.
  * max_len: a bound on lens, known to the host; it only decides how the keys
  * are split over the chip (0: not known, as for short prompts).  The
  * workspace must hold cdsl_op_tree_attention_workspace bytes for the same
  * arguments (0: none needed, or arguments that the call refuses); it needs no
- * initial contents.  Results do not
- * depend on other calls, and the same arguments give the same bits.  Errors:
- * EINVAL, ERANGE (n beyond CDSL_TREE_MAX with parents, batch * n * H of 2^24
- * or more), EDEVICE. */
+ * initial contents.  Results do not depend on other calls, and the same
+ * arguments give the same bits.  Errors: EINVAL, ERANGE (n beyond
+ * CDSL_TREE_MAX with parents, batch * n * H of 2^24 or more), EDEVICE. */
 size_t cdsl_op_tree_attention_workspace(int32_t batch, int32_t n, int32_t H,
                                         int32_t n_kv_heads, int32_t head_dim,
                                         int32_t max_len);

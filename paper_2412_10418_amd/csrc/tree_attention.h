@@ -20,11 +20,12 @@
 // for bf16 (exact down to 2^-31 of the largest).  The key codes are taken times
 // 2^-14 in turn, exact in f16, whose subnormals the products keep.
 // Probabilities times s_v can be of any size, so they stay bf16: three planes
-// (their 24 bits) for fp32, one (2^-8 of each, independent over the keys; the
-// result rounds by as much) for bf16.  Two planes would lose 2^-16 of each
-// probability: 2.5e-6 of the result, where fp32 products give 0.8e-6.  (A
-// second plane for bf16 would bring 0.0017 of the result instead of 0.0023, for
-// 10% more time where there are many rows.)
+// (their 24 bits) for fp32, where two would lose 2^-16 of each: 2.5e-6 of the
+// result, where fp32 products give 0.8e-6.  For bf16 two (2^-16 of each; 0.0017 of
+// the result in the mean square, its own rounding) with one tile of rows, where
+// the keys' bytes bound the time, and one (2^-8; 0.0023) with more rows, where the
+// second takes 6 to 24% longer (8 prompts of 8 nodes x 4 at 4096: 22.2 -> 23.6 us, 64
+// trees of 65 at 2048: 140 -> 155, two chunks of 512 over 32768: 685 -> 852).
 //
 // Three kernels.  Few rows (one or two tiles): the codes go from memory
 // straight to the registers of the wave that uses them, and the waves of a
@@ -325,27 +326,32 @@ __device__ __forceinline__ void q_planes(const float (&x)[8], float down, f16x8 
   }
 }
 
-// Probabilities times s_v as bf16 planes: one, rounded; or three by
-// truncation, 8 bits each, where each rest is exact.
+// Probabilities times s_v as bf16 planes: one, rounded; two, rounded (16 bits); or
+// three by truncation, 8 bits each.  Every rest is exact.
 template <int PP>
 __device__ __forceinline__ void p_planes(float (&w)[8], bf16x8 (&pf)[PP]) {
-  if constexpr (PP == 1) {
+  union {
+    unsigned u[4];
+    bf16x8 v;
+  } o;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) pf[0][e] = (bf16)w[e];
-  } else {
-    union {
-      unsigned u[4];
-      bf16x8 v;
-    } o;
+  for (int pl = 0; pl < PP; ++pl) {
 #pragma unroll
-    for (int pl = 0; pl < PP; ++pl) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (PP < 3) {
+        o.v[2 * e] = (bf16)w[2 * e];
+        o.v[2 * e + 1] = (bf16)w[2 * e + 1];
+      } else {
         o.u[e] = __builtin_amdgcn_perm(__float_as_uint(w[2 * e + 1]), __float_as_uint(w[2 * e]), 0x07060302);
-      pf[pl] = o.v;
-      if (pl + 1 < PP)
+      }
+    }
+    pf[pl] = o.v;
+    if (pl + 1 < PP) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] -= __uint_as_float(__float_as_uint(w[e]) & 0xffff0000u);
+      for (int e = 0; e < 8; ++e) {
+        const unsigned high = PP == 2 ? (e & 1 ? o.u[e / 2] : o.u[e / 2] << 16) : __float_as_uint(w[e]);
+        w[e] -= __uint_as_float(high & 0xffff0000u);
+      }
     }
   }
 }
@@ -357,11 +363,12 @@ __device__ __forceinline__ void store4(QT* o, f32x4 y) {
 }
 
 // One tile of 16 rows in a wave: lane (row lr = lane % 16, group lg = lane / 16).
-template <int HD, typename QT>
+// PLANES: of p s_v.
+template <int HD, typename QT, int PLANES>
 struct RowTile {
   static constexpr int S = HD / 32, DT = HD / 16;
   static constexpr int QP = sizeof(QT) == 4 ? 2 : 1;   // planes of q
-  static constexpr int PP = sizeof(QT) == 4 ? 3 : 1;   // planes of p s_v
+  static constexpr int PP = PLANES;
   f16x8 q[S][QP];
   float rm;              // what a score of the scaled q counts in log2 units
   f32x4 acc[DT];         // dims 16 t + 4 lg .. +3 of row lr
@@ -464,11 +471,11 @@ struct RowTile {
 
 // Scores of a page's two halves; dim step s, key codes k0 and k1.  Every
 // other product belongs to another sum, so that none waits for the one before.
-template <int HD, typename QT, int RPW>
-__device__ __forceinline__ void score_step(const RowTile<HD, QT> (&row)[RPW], int s, const f16x8& k0, const f16x8& k1,
+template <typename Row, int RPW>
+__device__ __forceinline__ void score_step(const Row (&row)[RPW], int s, const f16x8& k0, const f16x8& k1,
                                            f32x4 (&sc)[RPW][2]) {
 #pragma unroll
-  for (int pl = 0; pl < RowTile<HD, QT>::QP; ++pl)
+  for (int pl = 0; pl < Row::QP; ++pl)
 #pragma unroll
     for (int r = 0; r < RPW; ++r) {
       sc[r][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, row[r].q[s][pl], sc[r][0], 0, 0, 0);
@@ -477,11 +484,11 @@ __device__ __forceinline__ void score_step(const RowTile<HD, QT> (&row)[RPW], in
 }
 
 // O of the dim tiles d and d + 1, value codes v0 and v1.
-template <int HD, typename QT, int RPW>
-__device__ __forceinline__ void value_step(RowTile<HD, QT> (&row)[RPW], int d, const bf16x8& v0, const bf16x8& v1,
-                                           const bf16x8 (&pf)[RPW][RowTile<HD, QT>::PP]) {
+template <typename Row, int RPW>
+__device__ __forceinline__ void value_step(Row (&row)[RPW], int d, const bf16x8& v0, const bf16x8& v1,
+                                           const bf16x8 (&pf)[RPW][Row::PP]) {
 #pragma unroll
-  for (int pl = 0; pl < RowTile<HD, QT>::PP; ++pl)
+  for (int pl = 0; pl < Row::PP; ++pl)
 #pragma unroll
     for (int r = 0; r < RPW; ++r) {
       row[r].acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[r][pl], row[r].acc[d], 0, 0, 0);
@@ -491,11 +498,11 @@ __device__ __forceinline__ void value_step(RowTile<HD, QT> (&row)[RPW], int d, c
 
 // Planes of p s_v of every row tile of a wave, from a page's scores.
 // MASKED: the page holds nodes.
-template <bool MASKED, int HD, typename QT, int RPW>
-__device__ __forceinline__ void page_softmax(RowTile<HD, QT> (&row)[RPW], const f32x4 (&sc)[RPW][2], const f32x4 (&ks)[2],
+template <bool MASKED, typename Row, int RPW>
+__device__ __forceinline__ void page_softmax(Row (&row)[RPW], const f32x4 (&sc)[RPW][2], const f32x4 (&ks)[2],
                                              const f32x4 (&vs)[2], bool tree, int i0, int node0,
                                              const uint32_t* masks, int lg,
-                                             bf16x8 (&pf)[RPW][RowTile<HD, QT>::PP]) {
+                                             bf16x8 (&pf)[RPW][Row::PP]) {
 #pragma unroll
   for (int r = 0; r < RPW; ++r) {
     float s[8], v[8];
@@ -507,7 +514,7 @@ __device__ __forceinline__ void page_softmax(RowTile<HD, QT> (&row)[RPW], const 
     if constexpr (MASKED) {
       const unsigned vis = tree ? slots_of_tree(i0, masks + (row[r].node - node0) * kTreeWords)
                                 : slots_of_chain(i0, row[r].node);
-      RowTile<HD, QT>::hide(s, v, vis >> (4 * lg));
+      Row::hide(s, v, vis >> (4 * lg));
     }
     row[r].softmax(s, v, pf[r]);
   }
@@ -522,7 +529,7 @@ __device__ __forceinline__ void page_softmax(RowTile<HD, QT> (&row)[RPW], const 
 template <int HD, int FMT, typename QT, int RPW>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void tree_few_kernel(TreeAttnArgs a) {
   constexpr int KW = 4;
-  using Row = RowTile<HD, QT>;
+  using Row = RowTile<HD, QT, sizeof(QT) == 4 ? 3 : RPW == 1 ? 2 : 1>;
   constexpr int S = Row::S, DT = Row::DT;
   constexpr int UNIT = kvq_unit_bytes(HD);
   constexpr int SLOT = (2 + 4 * DT) * 64;    // floats a wave hands over per row tile
@@ -682,7 +689,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
 // 132 in bf16, 146 in fp32, a few of which then live in scratch outside it).
 template <int HD, int FMT, typename QT, int EU>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EU))) void tree_many_kernel(TreeAttnArgs a) {
-  using Row = RowTile<HD, QT>;
+  using Row = RowTile<HD, QT, sizeof(QT) == 4 ? 3 : 1>;
   constexpr int NT = 256, W = 4;
   constexpr int S = Row::S, DT = Row::DT;
   constexpr int UNIT = kvq_unit_bytes(HD);

@@ -60,7 +60,9 @@ def test_results_are_as_near_as_their_products(case, kind, fmt, outlier):
     that in the mean square: 16 x 0.3 x 1.4 x 2^-24 = 4e-7 of a probability; its exponential and the sums over the keys
     as much again: 1e-6 in all.  (Probabilities of 16 bits, 2^-16 at most, would give 2.5e-6; entries of q to 2^-25 of an
     outlier of 1e3 3e-5.)  bf16: beside the results' own rounding each probability is rounded, by itself and by half
-    a step, 2^-8 of it, at most, so in a sum of independent terms the mean square grows by 2^-16 of the results' at most."""
+    a step, 2^-8 of it, at most, so in a sum of independent terms the mean square grows by 2^-16 of the results' at most.
+    With 16 rows a KV head or fewer it is off by 2^-16 at most, and so is the result but for its own rounding (1% of which
+    is for the roundings that fall to the other side)."""
     from paper_2412_10418_amd import binding as bd
     rng = np.random.default_rng([case.B, case.n, 72])
     cache, lens, some, k, v = _filled(rng, case, fmt, quiet=5)
@@ -80,7 +82,12 @@ def test_results_are_as_near_as_their_products(case, kind, fmt, outlier):
         ref.append(o.ravel())
     off, own, ref = (rms(np.concatenate(x)) for x in (off, own, ref))
     print(f"{case.name} {kind} {fmt}: off by {off / ref:.3g} of the results, their own rounding {own / ref:.3g}", flush=True)
-    assert off <= 1e-6 * ref if kind == "f32" else off ** 2 <= own ** 2 + (2.0 ** -8 * ref) ** 2
+    if kind == "f32":
+        assert off <= 1e-6 * ref
+    elif case.kernel(kind, fmt).startswith("few1"):
+        assert off <= 1.01 * own + 2.0 ** -16 * ref
+    else:
+        assert off ** 2 <= own ** 2 + (2.0 ** -8 * ref) ** 2
 
 
 @pytest.mark.parametrize("V", [3001, 32768, 40001])
