@@ -286,8 +286,9 @@ __global__ __launch_bounds__(NT) void tree_sums_kernel(AcceptArgs a) {
 }
 
 // CHUNKS: V <= CHUNKS * CHUNK, the one launch (one chunk of registers takes 18 us
-// over 16384 ids and 27 for 45 prompts over 12368, where two take 22.5 and 35);
-// 0: the one after the rounds.
+// over 16384 ids and 27 for 45 prompts over 12368, where two take 22.5 and 35; two
+// fill the 128 registers, one value more lives in scratch); 0: the one after the
+// rounds.
 template <int CHUNKS>
 __global__ __launch_bounds__(NT) void tree_accept_kernel(AcceptArgs a) {
   constexpr bool HELD = CHUNKS > 0;
@@ -477,9 +478,12 @@ __global__ __launch_bounds__(NT) void tree_accept_kernel(AcceptArgs a) {
 int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
 
 // The more prompts, the longer the longest walk; the longer the rows, the more a
-// sum in the last launch costs.  With 2, 4 and 5 rounds: 8 trees over 65536 take
-// 21.6, 25.4 and 27.9 us, 8 over 128256 40.6, 31.2 and 33.6, 32 over 128256 71,
-// 55 and 50.
+// sum in the last launch costs.  Trees of 65 (us, with 2, 4 and 5 rounds):
+//   prompts         8                16                24                32
+//   35101    31.6 33.0 35.4   36.5 36.5 38.9   38.9 39.7 40.8   39.4 38.8 40.6
+//   65536    27.9 29.3 32.1   35.9 33.2 36.1   43.0 41.5 43.2   38.5 36.6 38.6
+//   128256   40.3 31.9 35.6   48.3 39.6 40.5   55.7 47.4 47.3   68.9 55.7 52.2
+// (how many children each draw rejects makes up to 10 us of them).
 int rounds_of(int B, int V) { return B >= 32 ? kRounds : B <= 16 && V <= 4 * CHUNK ? 2 : 4; }
 
 }  // namespace

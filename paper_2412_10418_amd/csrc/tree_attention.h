@@ -525,7 +525,10 @@ __device__ __forceinline__ void page_softmax(Row (&row)[RPW], const f32x4 (&sc)[
 // loop: the cache holds the codes in operand order (kvq_layout.h), 16 bytes a
 // lane, and the next page's loads are in flight while one is computed.  The
 // waves merge through LDS, key splits through a second kernel, both in a
-// fixed order.
+// fixed order.  (Two tiles of fp32 rows over heads of 128 take all 256 registers
+// and 9, over int8 16, more in scratch: stored and read around the loop, and one
+// of them in a page with nodes.  8 prompts of 8 nodes x 4 at 4096: 29.7 us, in bf16,
+// which needs none, 22.3.)
 template <int HD, int FMT, typename QT, int RPW>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void tree_few_kernel(TreeAttnArgs a) {
   constexpr int KW = 4;
@@ -686,7 +689,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
 // codes come in as 16 bytes a thread, two pages before they are needed, and go
 // to LDS as f16 (keys) and bf16 (values) in operand order.
 // EU: waves a SIMD at least.  Four leave 128 registers a lane (the loop likes
-// 132 in bf16, 146 in fp32, a few of which then live in scratch outside it).
+// 134 in bf16, 146 in fp32; of the latter 11 then live in scratch, outside the
+// loop but for one that a page with nodes reads).
 template <int HD, int FMT, typename QT, int EU>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EU))) void tree_many_kernel(TreeAttnArgs a) {
   using Row = RowTile<HD, QT, sizeof(QT) == 4 ? 3 : 1>;
@@ -826,7 +830,7 @@ struct WideTile {
 // tree_many_kernel with tiles of 32 rows (MFMA 32x32x16): half the matrix
 // instructions and LDS reads.  A matrix instruction keeps the SIMD from
 // issuing vector ones for about eight cycles whatever its size (a wave of
-// either beside a wave of vector work: 376 us for 16x16x32, 326 for 32x32x16,
+// products beside a wave of additions: 372 us for 16x16x32, 325 for 32x32x16,
 // where each alone takes 250), and the vector work of the softmax is as long
 // as the products (64 prompts x 8 KV heads of 256 rows at up to 2048 tokens: 119
 // us in bf16, 194 in fp32 over int8, where tiles of 16 take 127 and 201).
