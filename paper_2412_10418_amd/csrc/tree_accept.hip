@@ -107,7 +107,7 @@ __device__ __forceinline__ double weights(const Piece& p, const Piece& q, double
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (__builtin_isunordered(p.x[u][e], q.x[u][e])) s = NAN;
+        if (__builtin_isnan(p.x[u][e] - q.x[u][e])) s = NAN;   // one of them is, or both are infinite
   }
   return s;
 }

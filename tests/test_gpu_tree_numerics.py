@@ -115,3 +115,18 @@ def test_a_nan_in_the_draft_row_of_a_rejection(V, at, bad):
     f = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda()  # noqa: E731
     path, m, tok = bd.cdsl_op_tree_accept(f(p), f(q), _ints([[0, 5]]), _ints([[-1, 0]]), f([[0.9, 0.9]]), f([0.5]))
     assert path.tolist() == [[0, -1]] and m.tolist() == [1] and tok.tolist() == [-1]
+
+
+@pytest.mark.parametrize("V", [300, 20000, 40001])
+@pytest.mark.parametrize("at", [0, 17, 299])
+def test_infinities_of_a_rejection(V, at):
+    """One in the target's row, or in both at the same token, is a sum that is not finite; one in the draft's alone leaves
+    nothing of its token, and the draw is among the others."""
+    from paper_2412_10418_amd import binding as bd
+    f = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda()  # noqa: E731
+    for pi, qi, none in ((np.inf, 0, True), (np.inf, np.inf, True), (0, np.inf, False)):
+        p, q = np.full((1, 2, V), 1 / V, np.float32), np.full((1, 2, V), 1 / (2 * V), np.float32)
+        q[:, :, 5], p[0, 0, at], q[0, 0, at] = 1, pi, qi
+        path, m, tok = bd.cdsl_op_tree_accept(f(p), f(q), _ints([[0, 5]]), _ints([[-1, 0]]), f([[0.9, 0.9]]), f([0.0]))
+        assert path.tolist() == [[0, -1]] and m.tolist() == [1]
+        assert tok.tolist() == [-1 if none else 1 if at == 0 else 0]
