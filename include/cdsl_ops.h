@@ -4,8 +4,8 @@
  * The first part exports single kernels of the step: exactly those that
  * cdsl_rollout / cdsl_verify launch, on caller buffers.  The second part
  * (from cdsl_kvq on) serves callers that hold their own paged cache and draft
- * trees of tokens rather than chains: an 8-bit cache, the attention of a tree
- * over it, the tree's verification and the move of its accepted path.
+ * trees of tokens rather than chains: a cache in 8 or 4 bits, the attention of a
+ * tree over it, the tree's verification and the move of its accepted path.
  * All pointers are device pointers owned by the caller; calls are
  * asynchronous on `stream` (a hipStream_t, NULL = default stream) and return
  * CDSL_OK or a negative CDSL_E* code (see cdsl.h).  No call allocates.
@@ -109,11 +109,12 @@ int cdsl_op_soft_rows(const float* target_logits, const float* draft_logits,
                       const float* v, float* draft_lp, int32_t* res_ids,
                       float* res_lp, void* stream);
 
-/* ---- A drafted tree served from an 8-bit paged cache ----
+/* ---- A drafted tree served from an 8-bit or 4-bit paged cache ----
  *
  * The cache holds keys and values in 8 bits, a scale per token and KV head
  * (fp32): 2 * head_dim + 8 bytes a token and head, where the step's own cache
- * (fp32 values) takes 8 * head_dim.  Pages hold CDSL_KVQ_PAGE tokens; token
+ * (fp32 values) takes 8 * head_dim; or in 4 bits, a byte of scale per 32 dims:
+ * 17 / 16 * head_dim bytes.  Pages hold CDSL_KVQ_PAGE tokens; token
  * position x of prompt b lies on page table[b][x / 32], slot x % 32.  One
  * step over trees of drafted tokens is
  *   cdsl_op_kvq_write       the nodes' keys and values, per layer
@@ -132,6 +133,12 @@ int cdsl_op_soft_rows(const float* target_logits, const float* draft_logits,
  *                   2^-126; code = x / s to the nearest e4m3, ties to even
  * and the value is code * s.  A row with a NaN or an infinity has s = NaN: it
  * reads back as NaN, and rows that see it attend to NaN.
+ *   CDSL_KVQ_MXFP4  for each block of 32 dims of the row, with a = max |x| over
+ *                   the block: s = the smallest power of two with a <= 6 s, at
+ *                   least 2^-125, at most 2^125; code = x / s to the nearest of
+ *                   0, 1/2, 1, 3/2, 2, 3, 4 and 6, ties to the even code, at
+ *                   most 6 (where s is 2^125)
+ * A NaN or an infinity in one block is one in the whole row here too.
  *
  * Page ids are not checked on the host.  A position beyond the table, below
  * 0, or on a page id outside [0, pages) is never accessed: it is not written,
@@ -144,10 +151,10 @@ int cdsl_op_soft_rows(const float* target_logits, const float* draft_logits,
 #define CDSL_KVQ_PAGE 32
 #define CDSL_TREE_MAX 512          /* nodes of a tree that has parents */
 #define CDSL_ACCEPT_MAX_VOCAB (1 << 20)
-enum { CDSL_KVQ_INT8 = 0, CDSL_KVQ_E4M3 = 1 };
+enum { CDSL_KVQ_INT8 = 0, CDSL_KVQ_E4M3 = 1, CDSL_KVQ_MXFP4 = 4 };
 
 typedef struct cdsl_kvq {
-  void* pool;            /* device, cdsl_op_kvq_pool_bytes; needs no initial contents */
+  void* pool;            /* device, cdsl_op_kvq_pool_bytes_of; needs no initial contents */
   const int32_t* table;  /* device [batch][table_stride] page ids */
   int32_t n_layers;
   int32_t pages;         /* pages per layer */
@@ -155,14 +162,18 @@ typedef struct cdsl_kvq {
   int32_t head_dim;      /* 32, 64 or 128 */
   int32_t batch;         /* prompts (<= 65535) */
   int32_t table_stride;  /* pages per prompt (< 2^26) */
-  int32_t format;        /* CDSL_KVQ_INT8 or CDSL_KVQ_E4M3 */
+  int32_t format;        /* CDSL_KVQ_INT8, CDSL_KVQ_E4M3 or CDSL_KVQ_MXFP4 */
 } cdsl_kvq;
 
 /* Bytes of the pool: n_layers * pages * n_kv_heads units of
- * 64 * head_dim + 256 bytes, laid out [layer][page][head].  0 for arguments
- * out of range and pools of 2^62 bytes or more. */
+ * 64 * head_dim + 256 bytes (8 bits; CDSL_KVQ_MXFP4: 34 * head_dim), laid out
+ * [layer][page][head].  0 for arguments out of range and pools of 2^62 bytes or
+ * more.  The first form is that of the 8-bit formats. */
 size_t cdsl_op_kvq_pool_bytes(int32_t n_layers, int32_t pages,
                               int32_t n_kv_heads, int32_t head_dim);
+size_t cdsl_op_kvq_pool_bytes_of(int32_t n_layers, int32_t pages,
+                                 int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t format);
 
 /* Quantises rows into a layer of the cache.  K and V are
  * [batch][T][n_kv_heads][head_dim] of dtype CDSL_F32 or CDSL_BF16, heads and
@@ -202,6 +213,8 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V,
  * probabilities of a bf16 call, which are rounded to bf16 (to twice its bits
  * where n * H / n_kv_heads is 16 or less), and for entries of Q below 2^-15
  * (bf16: 2^-31) of their row's largest, which are off by up to 2^-39 of that.
+ * Over CDSL_KVQ_MXFP4 no entry of Q is off: it enters as it is, times keys as
+ * they are, and scale multiplies the sum.
  * They overflow as in fp32, before the division by the sum of the probabilities
  * (the largest of which counts 1 to 2^8) and with rows of Q scaled to entries
  * below 2: keys, and values times the number of keys, stay below 2^119.

@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(HERE, "_lib", "libcdsl.so")
 CDSL_OK, CDSL_EINVAL, CDSL_ERANGE, CDSL_ENOMEM, CDSL_EDEVICE, CDSL_ESTATE = 0, -1, -2, -3, -4, -5
 CDSL_F32, CDSL_BF16 = 0, 1
 CDSL_EPI_STORE, CDSL_EPI_RESIDUAL = 0, 1
-CDSL_KVQ_INT8, CDSL_KVQ_E4M3 = 0, 1
+CDSL_KVQ_INT8, CDSL_KVQ_E4M3, CDSL_KVQ_MXFP4 = 0, 1, 4
 CDSL_KVQ_PAGE, CDSL_TREE_MAX, CDSL_ACCEPT_MAX_VOCAB = 32, 512, 1 << 20
 ERR_NAMES = {0: "OK", -1: "EINVAL", -2: "ERANGE", -3: "ENOMEM", -4: "EDEVICE", -5: "ESTATE"}
 
@@ -34,7 +34,7 @@ EXPORTS = [
     "cdsl_prefix_lengths",
     "cdsl_free_prefix", "cdsl_destroy", "cdsl_last_error", "cdsl_profile_enable", "cdsl_profile_read",
     "cdsl_op_gemm_workspace", "cdsl_op_gemm", "cdsl_op_gemm_static", "cdsl_op_logit_rows",
-    "cdsl_op_kvq_pool_bytes", "cdsl_op_kvq_write", "cdsl_op_kvq_read", "cdsl_op_kvq_keep",
+    "cdsl_op_kvq_pool_bytes", "cdsl_op_kvq_pool_bytes_of", "cdsl_op_kvq_write", "cdsl_op_kvq_read", "cdsl_op_kvq_keep",
     "cdsl_op_tree_attention_workspace", "cdsl_op_tree_attention", "cdsl_op_tree_accept_workspace",
     "cdsl_op_tree_accept",
 ]
@@ -130,6 +130,7 @@ def lib():
         "cdsl_op_gemm_static": ([vp, vp, vp, i32, i32, i32, i32, i32, vp], i32),
         "cdsl_op_logit_rows": ([vp, i32, i32, vp, i32, vp, vp, vp, vp, vp], i32),
         "cdsl_op_kvq_pool_bytes": ([i32, i32, i32, i32], C.c_size_t),
+        "cdsl_op_kvq_pool_bytes_of": ([i32, i32, i32, i32, i32], C.c_size_t),
         "cdsl_op_kvq_write": ([vp, i32, vp, vp, i32, i32, i64, i64, i64, i64, vp, vp, vp], i32),
         "cdsl_op_kvq_read": ([vp, i32, vp, vp, i32, i32, vp, vp, vp], i32),
         "cdsl_op_kvq_keep": ([vp, vp, vp, vp, i32, vp, vp], i32),
@@ -273,9 +274,9 @@ def cdsl_op_soft_rows(target_logits: torch.Tensor, draft_logits: torch.Tensor, d
 
 
 # ---------------------------------------------------------------------------
-# a drafted tree served from an 8-bit paged cache
+# a drafted tree served from an 8-bit or 4-bit paged cache
 # ---------------------------------------------------------------------------
-_KVQ_FORMATS = {"int8": CDSL_KVQ_INT8, "e4m3": CDSL_KVQ_E4M3}
+_KVQ_FORMATS = {"int8": CDSL_KVQ_INT8, "e4m3": CDSL_KVQ_E4M3, "mxfp4": CDSL_KVQ_MXFP4}
 _ROW_TYPES = {torch.float32: CDSL_F32, torch.bfloat16: CDSL_BF16}
 
 
@@ -321,8 +322,8 @@ def _call(dev: int, fn, *args):
 
 
 class QuantCache:
-    """The 8-bit paged cache of a batch of prompts: pool [layers, pages, heads, unit bytes] (uint8, see
-    ``QuantCache.empty``), table [prompts, pages per prompt] (int32 page ids).  The calls see what is written into the
+    """The paged cache of a batch of prompts, in 8 bits (fmt "int8" or "e4m3") or 4 ("mxfp4"): pool [layers, pages,
+    heads, unit bytes] (uint8, see ``QuantCache.empty``), table [prompts, pages per prompt] (int32 page ids).  The calls see what is written into the
     two tensors; for other ones make another QuantCache."""
 
     __slots__ = ("_pool", "_table", "_head_dim", "_fmt", "batch", "n_kv_heads", "device", "_c", "_ref")
@@ -338,8 +339,9 @@ class QuantCache:
             raise ValueError("pool must be [layers, pages, heads, unit], table [prompts, pages]")
         layers, pages, heads, unit = shape = pool.shape
         batch, stride = table.shape
-        if unit != 64 * head_dim + 256:
-            raise ValueError(f"a unit has 64 * head_dim + 256 = {64 * head_dim + 256} bytes, the pool {unit}")
+        want = 34 * head_dim if fmt == "mxfp4" else 64 * head_dim + 256
+        if unit != want:
+            raise ValueError(f"a unit of {fmt} at heads of {head_dim} has {want} bytes, the pool {unit}")
         dev = pool.get_device()
         if dev < 0:
             raise ValueError("pool must be a device tensor")
@@ -350,9 +352,11 @@ class QuantCache:
         self.batch, self.n_kv_heads, self.device = batch, heads, dev
 
     @staticmethod
-    def empty(layers: int, pages: int, n_kv_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
-        """A pool without contents."""
-        n = lib().cdsl_op_kvq_pool_bytes(layers, pages, n_kv_heads, head_dim)
+    def empty(layers: int, pages: int, n_kv_heads: int, head_dim: int, device="cuda", fmt: str = "int8") -> torch.Tensor:
+        """A pool without contents (the 8-bit formats have units of one size)."""
+        if fmt not in _KVQ_FORMATS:
+            raise ValueError(f"fmt must be one of {sorted(_KVQ_FORMATS)}, got {fmt!r}")
+        n = lib().cdsl_op_kvq_pool_bytes_of(layers, pages, n_kv_heads, head_dim, _KVQ_FORMATS[fmt])
         if n == 0:
             raise ValueError("pool sizes must be positive and head_dim 32, 64 or 128")
         return torch.empty((layers, pages, n_kv_heads, n // (layers * pages * n_kv_heads)), dtype=torch.uint8,

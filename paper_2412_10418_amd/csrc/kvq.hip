@@ -1,5 +1,6 @@
 // The 8-bit paged cache: rows quantised as they are written, read back, and
-// the kept path of a tree moved to the front of the tree's slots.
+// the kept path of a tree moved to the front of the tree's slots.  (The 4-bit one:
+// kvq_fp4.hip.)
 //
 // One scale per (token, KV head) row x of hd values, a = max |x|:
 //   int8  s = max(a / 127, 2^-126) (rounded to fp32), code = x / s to the
@@ -11,6 +12,7 @@
 // its code's rounding alone.
 #include <type_traits>
 
+#include "kvq_rows.h"
 #include "tree.h"
 
 namespace cdsl {
@@ -103,23 +105,9 @@ __device__ __forceinline__ void decode4(unsigned w, float s, float (&y)[4]) {
   }
 }
 
-// Bytes (t, e) -> (e, t) of four words.
-__device__ __forceinline__ void transpose4(const unsigned (&w)[4], unsigned (&o)[4]) {
-  const unsigned a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400);
-  const unsigned c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
-  o[0] = __builtin_amdgcn_perm(b, a, 0x05040100);
-  o[1] = __builtin_amdgcn_perm(b, a, 0x07060302);
-  o[2] = __builtin_amdgcn_perm(d, c, 0x05040100);
-  o[3] = __builtin_amdgcn_perm(d, c, 0x07060302);
-}
-
 // Maximum over groups of LANES lanes (8, 16 or 32): within quads, halves of a
 // row, rows of 16, then the two rows; vector instructions only (shuffles
 // through LDS, 40 a thread, took 6 us of 42 at 24 prompts of up to 2047).
-template <int CTRL>
-__device__ __forceinline__ unsigned max_moved(unsigned a) {
-  return max(a, (unsigned)__builtin_amdgcn_update_dpp(0, (int)a, CTRL, 0xf, 0xf, false));
-}
 template <int LANES>
 __device__ __forceinline__ unsigned group_max(unsigned a) {
   a = max_moved<0xB1>(a);                             // quad_perm 1 0 3 2
@@ -133,11 +121,6 @@ __device__ __forceinline__ unsigned group_max(unsigned a) {
   }
   return a;
 }
-
-// Where word w of a unit's codes stands in LDS: the sixteen 16-byte chunks of a
-// row of 64 words are permuted by the row, so that neither the order of the
-// rows (dims along the lanes) nor that of the unit meets one bank often.
-__device__ __forceinline__ int banked(int w) { return w ^ ((w >> 6 & 15) << 2); }
 
 // Threads of a workgroup: a task is four slots x four dims of the keys or of
 // the values (16 hd / 4 tasks a unit), so that a quarter-row load or store of
@@ -292,12 +275,6 @@ __global__ __launch_bounds__(kvq_threads<HD>()) void kvq_read_kernel(KvqView c, 
       else *(bf16x4*)o = (bf16x4){(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
     }
   }
-}
-
-// The pointer that another lane holds.
-template <typename P>
-__device__ __forceinline__ P* ptr_of_lane(P* p, int lane) {
-  return (P*)__shfl((long long)p, lane, 64);
 }
 
 // Moves of single tokens.  One wave per (layer, KV head, prompt); entry i of the
@@ -464,6 +441,7 @@ hipError_t rows_format(const KvqView& c, const KvqRows& r, bool write, hipStream
 
 hipError_t rows_any(const KvqView& c, const KvqRows& r, bool write, hipStream_t st) {
   if (c.B == 0 || r.T == 0) return hipSuccess;
+  if (c.format == kMxfp4) return fp4_rows_launch(c, r, write, st);
   switch (c.hd) {
     case 32: return rows_format<32>(c, r, write, st);
     case 64: return rows_format<64>(c, r, write, st);
@@ -480,6 +458,7 @@ hipError_t kvq_read_launch(const KvqView& c, const KvqRows& r, hipStream_t st) {
 hipError_t kvq_keep_launch(const KvqView& c, int n_layers, long long layer_bytes, const int* lens, const int* path,
                            const int* n_path, int n, int* new_lens, hipStream_t st) {
   if (c.B == 0) return hipSuccess;
+  if (c.format == kMxfp4) return fp4_keep_launch(c, n_layers, layer_bytes, lens, path, n_path, n, new_lens, st);
   const dim3 grid((unsigned)(n_layers * c.Hkv), (unsigned)c.B);
   switch (c.hd) {
     case 32: kvq_keep_kernel<32><<<grid, 64, 0, st>>>(c, layer_bytes, lens, path, n_path, n, new_lens); break;

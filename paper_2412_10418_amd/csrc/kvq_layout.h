@@ -1,5 +1,5 @@
-// The 8-bit paged cache: where its bytes stand, which page a position lies
-// on, and which slots of a page a node sees.  Plain C++ without HIP headers,
+// The 8-bit and 4-bit paged cache: where its bytes stand, which page a position
+// lies on, and which slots of a page a node sees.  Plain C++ without HIP headers,
 // so that it also builds as host-only code for unit tests under the address
 // and undefined-behaviour sanitizers.
 //
@@ -10,6 +10,16 @@
 // lanes:
 //   keys    [dim / 32][(dim % 32) / 8][slot % 16][slot / 16][dim % 8]
 //   values  [dim / 32][(slot % 16) / 4][dim % 16][(dim % 32) / 16][slot / 16][slot % 4]
+// In 4 bits a unit holds the codes of 32 keys, those of 32 values, a byte of
+// scale for every 32 dims of a key, and the same of the values.  A byte of codes
+// is two dims of one token (the even one in the lower half), so that no two
+// tokens share a byte, and 64 dims fill a lane's 16 bytes (heads of 32 dims: its
+// 8).  With lane = (dim % 32) / 8 * 16 + slot % 16 for keys, and (slot % 16) / 4 *
+// 16 + dim % 32 / 2 for values:
+//   keys          [dim / 64][lane][dim / 32 % 2][slot / 16][dim % 8 / 2]
+//   values        [dim / 64][lane][dim / 32 % 2][slot / 16][slot % 4]
+//   key scales    [dim / 64][slot % 16][dim / 32 % 2][slot / 16]
+//   value scales  [dim / 64][(slot % 16) / 4][dim / 32 % 2][slot / 16][slot % 4]
 #pragma once
 
 #include <stdint.h>
@@ -23,9 +33,13 @@
 namespace cdsl {
 
 constexpr int kPage = 32;
-enum KvqFormat { kInt8 = 0, kE4M3 = 1 };
+enum KvqFormat { kInt8 = 0, kE4M3 = 1, kMxfp4 = 4 };
 
-CDSL_KVQ_HD constexpr int kvq_unit_bytes(int hd) { return 2 * kPage * hd + 8 * kPage; }
+CDSL_KVQ_HD constexpr int kvq_unit_bytes(int hd) { return 2 * kPage * hd + 8 * kPage; }   // 8-bit formats
+CDSL_KVQ_HD constexpr int fp4_unit_bytes(int hd) { return 34 * hd; }
+CDSL_KVQ_HD constexpr int kvq_unit_bytes(int hd, int format) {
+  return format == kMxfp4 ? fp4_unit_bytes(hd) : kvq_unit_bytes(hd);
+}
 CDSL_KVQ_HD constexpr int kvq_key_at(int slot, int dim) {
   return dim / 32 * 1024 + dim % 32 / 8 * 256 + slot % 16 * 16 + slot / 16 * 8 + dim % 8;
 }
@@ -35,6 +49,25 @@ CDSL_KVQ_HD constexpr int kvq_value_at(int hd, int slot, int dim) {
 }
 CDSL_KVQ_HD constexpr int kvq_key_scale_at(int hd, int slot) { return 2 * kPage * hd + 4 * slot; }
 CDSL_KVQ_HD constexpr int kvq_value_scale_at(int hd, int slot) { return 2 * kPage * hd + 4 * kPage + 4 * slot; }
+
+// 4 bits.  Blocks of 32 dims that share a lane's bytes: two, one in heads of 32.
+CDSL_KVQ_HD constexpr int fp4_pair(int hd) { return hd > 32 ? 2 : 1; }
+// The byte of dims dim (even) and dim + 1 of a key or a value, and the scale of
+// its block.
+CDSL_KVQ_HD constexpr int fp4_key_at(int hd, int slot, int dim) {
+  return dim / 64 * 1024 + (dim % 32 / 8 * 16 + slot % 16) * 8 * fp4_pair(hd) + dim / 32 % 2 * 8 + slot / 16 * 4 +
+         dim % 8 / 2;
+}
+CDSL_KVQ_HD constexpr int fp4_value_at(int hd, int slot, int dim) {
+  return 16 * hd + dim / 64 * 1024 + (slot % 16 / 4 * 16 + dim % 32 / 2) * 8 * fp4_pair(hd) + dim / 32 % 2 * 8 +
+         slot / 16 * 4 + slot % 4;
+}
+CDSL_KVQ_HD constexpr int fp4_key_scale_at(int hd, int slot, int dim) {
+  return 32 * hd + dim / 64 * 64 + slot % 16 * 2 * fp4_pair(hd) + dim / 32 % 2 * 2 + slot / 16;
+}
+CDSL_KVQ_HD constexpr int fp4_value_scale_at(int hd, int slot, int dim) {
+  return 33 * hd + dim / 64 * 64 + slot % 16 / 4 * 8 * fp4_pair(hd) + dim / 32 % 2 * 8 + slot / 16 * 4 + slot % 4;
+}
 
 struct KvqView {
   uint8_t* pool;           // base of the layer (keep: of layer 0)
@@ -48,7 +81,7 @@ CDSL_KVQ_HD uint8_t* kvq_unit_of(const KvqView& c, int b, long long p, int h) {
   if (p < 0 || p >= c.table_stride) return nullptr;
   const int id = c.table[(long long)b * c.table_stride + p];
   if (id < 0 || id >= c.pages) return nullptr;
-  return c.pool + ((long long)id * c.Hkv + h) * kvq_unit_bytes(c.hd);
+  return c.pool + ((long long)id * c.Hkv + h) * kvq_unit_bytes(c.hd, c.format);
 }
 
 // Positions [beg, end) of prompt b's run of T rows (null: from 0, all T).

@@ -1874,7 +1874,7 @@ int cdsl_op_lm_head_rows(const float* A, const void* B, int32_t M, int32_t V, in
 }
 
 // ---------------------------------------------------------------------------
-// a drafted tree served from an 8-bit paged cache (include/cdsl_ops.h)
+// a drafted tree served from an 8-bit or 4-bit paged cache (include/cdsl_ops.h)
 // ---------------------------------------------------------------------------
 namespace {
 
@@ -1886,6 +1886,8 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 // one of the strides (in elements) that must keep rows 16-byte aligned
 bool aligned_stride(int64_t s, int32_t dtype) { return s * (dtype == CDSL_BF16 ? 2 : 4) % 16 == 0; }
 
+bool kvq_format(int32_t f) { return f == CDSL_KVQ_INT8 || f == CDSL_KVQ_E4M3 || f == CDSL_KVQ_MXFP4; }
+
 // CDSL_OK, or the error of a cache descriptor
 int kvq_check(const cdsl_kvq* c) {
   if (!c || !c->pool || (!c->table && c->batch != 0))
@@ -1894,18 +1896,18 @@ int kvq_check(const cdsl_kvq* c) {
     return fail(nullptr, CDSL_EINVAL, "bad cache sizes");
   if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128)
     return fail(nullptr, CDSL_EINVAL, "head_dim must be 32, 64 or 128");
-  if (c->format != CDSL_KVQ_INT8 && c->format != CDSL_KVQ_E4M3) return fail(nullptr, CDSL_EINVAL, "bad cache format");
+  if (!kvq_format(c->format)) return fail(nullptr, CDSL_EINVAL, "bad cache format");
   if (!aligned16(c->pool)) return fail(nullptr, CDSL_EINVAL, "the pool must be 16-byte aligned");
   if (c->batch > 65535) return fail(nullptr, CDSL_ERANGE, "more than 65535 prompts");
   // positions and the ends of their pages are ints in the kernels
   if (c->table_stride >= (1 << 26)) return fail(nullptr, CDSL_ERANGE, "a table holds fewer than 2^26 pages a prompt");
-  if (cdsl_op_kvq_pool_bytes(c->n_layers, c->pages, c->n_kv_heads, c->head_dim) == 0)
+  if (cdsl_op_kvq_pool_bytes_of(c->n_layers, c->pages, c->n_kv_heads, c->head_dim, c->format) == 0)
     return fail(nullptr, CDSL_ERANGE, "pool beyond 2^62 bytes");
   return CDSL_OK;
 }
 
 long long kvq_layer_bytes(const cdsl_kvq* c) {
-  return (long long)c->pages * c->n_kv_heads * kvq_unit_bytes(c->head_dim);
+  return (long long)c->pages * c->n_kv_heads * kvq_unit_bytes(c->head_dim, c->format);
 }
 
 KvqView kvq_view(const cdsl_kvq* c, int32_t layer) {
@@ -1944,8 +1946,13 @@ int launched(hipError_t e) {
 extern "C" {
 
 size_t cdsl_op_kvq_pool_bytes(int32_t n_layers, int32_t pages, int32_t n_kv_heads, int32_t head_dim) {
+  return cdsl_op_kvq_pool_bytes_of(n_layers, pages, n_kv_heads, head_dim, CDSL_KVQ_INT8);
+}
+
+size_t cdsl_op_kvq_pool_bytes_of(int32_t n_layers, int32_t pages, int32_t n_kv_heads, int32_t head_dim, int32_t format) {
   if (n_layers <= 0 || pages <= 0 || n_kv_heads <= 0 || (head_dim != 32 && head_dim != 64 && head_dim != 128)) return 0;
-  const unsigned __int128 bytes = (unsigned __int128)n_layers * pages * n_kv_heads * kvq_unit_bytes(head_dim);
+  if (!kvq_format(format)) return 0;
+  const unsigned __int128 bytes = (unsigned __int128)n_layers * pages * n_kv_heads * kvq_unit_bytes(head_dim, format);
   return bytes >> 62 ? 0 : (size_t)bytes;
 }
 

@@ -1,6 +1,7 @@
-// Internal interface of the 8-bit paged cache (kvq.hip), the attention of a
-// token tree over it (tree_attention.h, an instance file per head dimension) and
-// the tree's verification (tree_accept.hip).
+// Internal interface of the 8-bit paged cache (kvq.hip) and the 4-bit one
+// (kvq_fp4.hip), the attention of a token tree over them (tree_attention.h,
+// tree_attention_fp4.h, an instance file per head dimension) and the tree's
+// verification (tree_accept.hip).
 #pragma once
 #include "common.h"
 #include "kvq_layout.h"
@@ -23,6 +24,10 @@ hipError_t kvq_write_launch(const KvqView& c, const KvqRows& r, hipStream_t st);
 hipError_t kvq_read_launch(const KvqView& c, const KvqRows& r, hipStream_t st);
 hipError_t kvq_keep_launch(const KvqView& c, int n_layers, long long layer_bytes, const int* lens, const int* path,
                            const int* n_path, int n, int* new_lens, hipStream_t st);
+// the 4-bit cache's part of them
+hipError_t fp4_rows_launch(const KvqView& c, const KvqRows& r, bool write, hipStream_t st);
+hipError_t fp4_keep_launch(const KvqView& c, int n_layers, long long layer_bytes, const int* lens, const int* path,
+                           const int* n_path, int n, int* new_lens, hipStream_t st);
 
 struct TreeAttnArgs {
   KvqView c;
@@ -42,6 +47,9 @@ struct TreeAttnArgs {
 };
 
 hipError_t tree_attn_launch(TreeAttnArgs a, const TreeAttnPlan& p, int dtype, void* workspace, hipStream_t st);
+hipError_t fp4_attn_hd32(const TreeAttnArgs& a, const TreeAttnPlan& p, int dtype, hipStream_t st);
+hipError_t fp4_attn_hd64(const TreeAttnArgs& a, const TreeAttnPlan& p, int dtype, hipStream_t st);
+hipError_t fp4_attn_hd128(const TreeAttnArgs& a, const TreeAttnPlan& p, int dtype, hipStream_t st);
 
 constexpr int kAcceptMaxVocab = 1 << 20;
 

@@ -1,5 +1,5 @@
 // Tree attention over the 8-bit cache: head dimension 128, and the dispatch over
-// head dimensions.
+// formats and head dimensions.
 #include "tree_attention.h"
 
 namespace cdsl {
@@ -16,6 +16,14 @@ hipError_t tree_attn_launch(TreeAttnArgs a, const TreeAttnPlan& p, int dtype, vo
   a.wg_tiles = p.wg_tiles;
   a.part_o = (float*)workspace;
   a.part_ml = a.part_o + (size_t)p.slots * a.n * a.H * a.c.hd;
+  if (a.c.format == kMxfp4) {
+    switch (a.c.hd) {
+      case 32: return fp4_attn_hd32(a, p, dtype, st);
+      case 64: return fp4_attn_hd64(a, p, dtype, st);
+      case 128: return fp4_attn_hd128(a, p, dtype, st);
+    }
+    return hipErrorInvalidValue;
+  }
   switch (a.c.hd) {
     case 32: return tree_attn_hd32(a, p, dtype, st);
     case 64: return tree_attn_hd64(a, p, dtype, st);

@@ -25,12 +25,16 @@ struct TreeAttnPlan {
 
 // dtype: 0 fp32, 1 bf16.  fp32 over e4m3 (heads of 128) is as fast in tiles of 16
 // rows (188 us) as of 32 (190).
-constexpr bool tree_may_be_wide(int hd, int dtype, int format) { return !(hd == 128 && dtype == 0 && format == kE4M3); }
+constexpr bool tree_may_be_wide(int hd, int dtype, int format) {
+  return format != kMxfp4 && !(hd == 128 && dtype == 0 && format == kE4M3);
+}
 
 // Four workgroups a CU where there are as many; fewer are faster in three (64
 // trees of 65 at 2048 in bf16: 152 -> 146 us; 16 of them: 56 -> 61).  Heads of 64
 // gain nothing by it, fp32 over int8 loses 5% (231 -> 243).
-constexpr bool tree_may_be_four(int hd, int dtype, int format) { return hd == 128 && (dtype == 1 || format == kE4M3); }
+constexpr bool tree_may_be_four(int hd, int dtype, int format) {
+  return format != kMxfp4 && hd == 128 && (dtype == 1 || format == kE4M3);
+}
 
 inline TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max_len, int dtype, int format) {
   TreeAttnPlan p{};
