@@ -284,6 +284,74 @@ int cdsl_op_kvq_keep(const cdsl_kvq* cache, const int32_t* lens,
                      const int32_t* path, const int32_t* n_path, int32_t n,
                      int32_t* new_lens, void* stream);
 
+/* ---- Pages that prompts share ----
+ *
+ * The calls above take a table as it is.  These make it, for a cache of any
+ * format: table [batch][table_stride] is the caller's array that cache->table
+ * stands for (writable here; cache->table itself is not read), refs [pages] counts
+ * the entries that hold each page.  An entry holds a page if it is one, in
+ * [0, pages); -1 is written where it holds none.  A page of refs 0 is free, one
+ * above 1 is shared; a page is one in all layers.  A table of -1s and refs of 0s
+ * are the start; after that only these calls change them.  (Counts that do not fit
+ * the table give other pages than wanted, never an access outside the arrays.)
+ *
+ * A batch of beams goes on from their chosen one with
+ *   cdsl_op_pages_fork      beams' tables := the chosen one's, nothing copied
+ *   cdsl_op_pages_reserve   pages of their own for what each writes next
+ * then writes, attends and keeps as above, and gives back what a prompt no longer
+ * needs with cdsl_op_pages_free.  What goes where does not depend on the order in
+ * which the chip works.  The calls allocate nothing and may be captured into a
+ * graph; two that work on one table, refs or pool must not overlap.
+ * Workspaces: cdsl_op_pages_workspace bytes are enough for each call (max_count:
+ * of the reserve; 0: of the others), without initial contents; 0 for arguments
+ * out of range.  Fork needs one beyond 512 prompts only, free and copy none.
+ * Errors of all: EINVAL (also arrays that overlap), ERANGE (more than 2^30 pages,
+ * pages of 2^34 bytes, and as for cdsl_kvq), EDEVICE. */
+size_t cdsl_op_pages_workspace(int32_t batch, int32_t table_stride,
+                               int32_t pages, int32_t max_count);
+
+/* Prompt b holds the pages that prompt parents[b] held before the call; those of
+ * its own that nobody else holds become free.  parents[b] = b: as it was; outside
+ * [0, batch): none. */
+int cdsl_op_pages_fork(const cdsl_kvq* cache, int32_t* table, int32_t* refs,
+                       const int32_t* parents, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* Room for count[b] tokens (clamped to 0..max_count) behind the lens[b] (below 0:
+ * 0) that prompt b has, on pages that no other entry holds.  An entry of theirs
+ * without a page gets one.  One whose page is shared gets another in its place, and
+ * the page's contents if tokens before lens[b] lie on it; but where all that hold
+ * a page leave it in this call, the first of them keeps it.  The pages handed out
+ * are the lowest free ones, to the prompts in their order and each one's entries
+ * in theirs; when they run out, the remaining entries stay as they are.  got[b]
+ * receives how many of the tokens have room: less than count[b] where free pages
+ * or the table end.  What lies behind them must not be written.
+ * Errors: ERANGE also for batch * (max_count / 32 + 2) beyond 2^30. */
+int cdsl_op_pages_reserve(const cdsl_kvq* cache, int32_t* table, int32_t* refs,
+                          const int32_t* lens, const int32_t* count,
+                          int32_t max_count, int32_t* got, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Prompt b gives back its pages behind its first lens[b] tokens (below 0: 0). */
+int cdsl_op_pages_free(const cdsl_kvq* cache, int32_t* table, int32_t* refs,
+                       const int32_t* lens, void* stream);
+
+/* The U used pages become the first U: the highest used one moves to the lowest
+ * free one, and so on, in all layers, table and refs with it.  used [1] receives
+ * U.  Pages from U on hold anything. */
+int cdsl_op_pages_compact(const cdsl_kvq* cache, int32_t* table, int32_t* refs,
+                          int32_t* used, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Copies page src[i] of one pool to page dst[i] of another (or the same), in all
+ * layers, i < n; a pair with an id outside its pool is passed over.  The caches
+ * have one format and the same layers and heads (pages, and tables, which are not
+ * read, may differ).  A page that is written must be no other pair's dst or, in
+ * one pool, src. */
+int cdsl_op_pages_copy(const cdsl_kvq* from, const int32_t* src,
+                       const cdsl_kvq* to, const int32_t* dst, int32_t n,
+                       void* stream);
+
 #ifdef __cplusplus
 }
 #endif

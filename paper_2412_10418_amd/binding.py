@@ -37,6 +37,8 @@ EXPORTS = [
     "cdsl_op_kvq_pool_bytes", "cdsl_op_kvq_pool_bytes_of", "cdsl_op_kvq_write", "cdsl_op_kvq_read", "cdsl_op_kvq_keep",
     "cdsl_op_tree_attention_workspace", "cdsl_op_tree_attention", "cdsl_op_tree_accept_workspace",
     "cdsl_op_tree_accept",
+    "cdsl_op_pages_workspace", "cdsl_op_pages_fork", "cdsl_op_pages_reserve", "cdsl_op_pages_free",
+    "cdsl_op_pages_compact", "cdsl_op_pages_copy",
 ]
 
 
@@ -140,6 +142,14 @@ def lib():
         "cdsl_op_tree_accept_workspace": ([i32, i32, i32], C.c_size_t),
         "cdsl_op_tree_accept": ([vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, C.c_size_t, vp], i32),
     }
+    sig.update({
+        "cdsl_op_pages_workspace": ([i32, i32, i32, i32], C.c_size_t),
+        "cdsl_op_pages_fork": ([vp, vp, vp, vp, vp, C.c_size_t, vp], i32),
+        "cdsl_op_pages_reserve": ([vp, vp, vp, vp, vp, i32, vp, vp, C.c_size_t, vp], i32),
+        "cdsl_op_pages_free": ([vp, vp, vp, vp, vp], i32),
+        "cdsl_op_pages_compact": ([vp, vp, vp, vp, vp, C.c_size_t, vp], i32),
+        "cdsl_op_pages_copy": ([vp, vp, vp, vp, i32, vp], i32),
+    })
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
         fn.argtypes = args
@@ -458,6 +468,69 @@ def cdsl_op_kvq_keep(cache: QuantCache, lens: torch.Tensor, path: torch.Tensor, 
           _of(path, (B, path.shape[1]), torch.int32, dev, "path"), _of(n_path, (B,), torch.int32, dev, "n_path"),
           path.shape[1], new.data_ptr())
     return new
+
+
+# ---------------------------------------------------------------------------
+# pages that prompts share
+# ---------------------------------------------------------------------------
+def _pages(cache: QuantCache, refs: torch.Tensor):
+    """Pointers of a cache's table, which these calls change, and of the pages' counts."""
+    return cache.table.data_ptr(), _of(refs, (cache.pool.shape[1],), torch.int32, cache.device, "refs")
+
+
+def _pages_workspace(cache: QuantCache, max_count: int):
+    need = lib().cdsl_op_pages_workspace(cache.batch, cache.table.shape[1], cache.pool.shape[1], max_count)
+    return torch.empty(need, dtype=torch.uint8, device=cache.pool.device) if need else None, need
+
+
+def cdsl_op_pages_fork(cache: QuantCache, refs: torch.Tensor, parents: torch.Tensor) -> None:
+    """Prompt b holds the pages that prompt parents[b] held (outside [0, B): none).  Changes cache.table and refs
+    [pages], the entries that hold each page."""
+    table, r = _pages(cache, refs)
+    ws, need = _pages_workspace(cache, 0) if cache.batch > 512 else (None, 0)
+    _call(cache.device, lib().cdsl_op_pages_fork, cache._ref, table, r, _ints(parents, (cache.batch,), cache.device, "parents"),
+          ws.data_ptr() if need else None, need)
+
+
+def cdsl_op_pages_reserve(cache: QuantCache, refs: torch.Tensor, lens: torch.Tensor, count: torch.Tensor,
+                          max_count: int) -> torch.Tensor:
+    """Pages of their own for count[b] <= max_count tokens behind lens[b]; a shared page with tokens on it is copied.
+    Returns how many tokens of each prompt have room [B]."""
+    dev, B = cache.device, cache.batch
+    table, r = _pages(cache, refs)
+    got = torch.empty(B, dtype=torch.int32, device=refs.device)
+    ws, need = _pages_workspace(cache, max_count)
+    _call(dev, lib().cdsl_op_pages_reserve, cache._ref, table, r, _of(lens, (B,), torch.int32, dev, "lens"),
+          _of(count, (B,), torch.int32, dev, "count"), max_count, got.data_ptr(), ws.data_ptr() if need else None, need)
+    return got
+
+
+def cdsl_op_pages_free(cache: QuantCache, refs: torch.Tensor, lens: torch.Tensor) -> None:
+    """Prompt b gives back its pages behind its first lens[b] tokens."""
+    table, r = _pages(cache, refs)
+    _call(cache.device, lib().cdsl_op_pages_free, cache._ref, table, r,
+          _of(lens, (cache.batch,), torch.int32, cache.device, "lens"))
+
+
+def cdsl_op_pages_compact(cache: QuantCache, refs: torch.Tensor) -> torch.Tensor:
+    """Moves the used pages to the front of the pool; returns their number (a scalar on the device)."""
+    table, r = _pages(cache, refs)
+    used = torch.empty((), dtype=torch.int32, device=refs.device)
+    ws, need = _pages_workspace(cache, 0)
+    _call(cache.device, lib().cdsl_op_pages_compact, cache._ref, table, r, used.data_ptr(), ws.data_ptr() if need else None, need)
+    return used
+
+
+def cdsl_op_pages_copy(cache: QuantCache, src: torch.Tensor, to: QuantCache, dst: torch.Tensor) -> None:
+    """Pages src [n] of cache's pool to pages dst [n] of to's, in all layers."""
+    dev = cache.device
+    if src.dim() != 1:
+        raise ValueError("src must be [n]")
+    if to.device != dev:
+        raise ValueError(f"both pools must be on device {dev}")
+    n = src.shape[0]
+    _call(dev, lib().cdsl_op_pages_copy, cache._ref, _of(src, (n,), torch.int32, dev, "src"), to._ref,
+          _of(dst, (n,), torch.int32, dev, "dst"), n)
 
 
 # ---------------------------------------------------------------------------

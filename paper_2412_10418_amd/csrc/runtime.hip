@@ -24,6 +24,7 @@
 #include "common.h"
 #include "gemm.h"
 #include "kernels.h"
+#include "pages.h"
 #include "tree.h"
 
 using namespace cdsl;
@@ -1937,6 +1938,39 @@ bool overlap(const int32_t* a, int64_t na, const int32_t* b, int64_t nb) {
   return (uintptr_t)a < (uintptr_t)b + 4 * nb && (uintptr_t)b < (uintptr_t)a + 4 * na;
 }
 
+// CDSL_OK, or the error of a call that gives or takes pages
+int pages_check(const cdsl_kvq* c, const int32_t* table, const int32_t* refs) {
+  const int rc = kvq_check(c);
+  if (rc != CDSL_OK) return rc;
+  if ((!table || !refs) && c->batch != 0) return fail(nullptr, CDSL_EINVAL, "null table or refs");
+  // sums over the pages, and the words of one, are ints in the kernels
+  if (c->pages > (1 << 30)) return fail(nullptr, CDSL_ERANGE, "more than 2^30 pages");
+  if (kvq_layer_bytes(c) / c->pages >> 34) return fail(nullptr, CDSL_ERANGE, "pages of 2^34 bytes or more");
+  if (overlap(table, (int64_t)c->batch * c->table_stride, refs, c->pages))
+    return fail(nullptr, CDSL_EINVAL, "table and refs must not overlap");
+  return CDSL_OK;
+}
+
+// whether n ints from x on are none of the table and none of refs
+bool apart(const cdsl_kvq* c, const int32_t* table, const int32_t* refs, const int32_t* x, int64_t n) {
+  return !overlap(x, n, table, (int64_t)c->batch * c->table_stride) && !overlap(x, n, refs, c->pages);
+}
+
+PagesArgs pages_args(const cdsl_kvq* c, int32_t* table, int32_t* refs) {
+  const long long layer = kvq_layer_bytes(c);
+  return PagesArgs{table, refs, c->batch, c->table_stride, c->pages, (uint8_t*)c->pool, c->n_layers, layer, layer / c->pages};
+}
+
+bool pages_entries_fit(int32_t batch, int32_t max_count) {
+  return (long long)batch * (max_count / kPage + 2LL) <= (1 << 30);
+}
+
+int workspace_check(const void* workspace, size_t have, size_t need) {
+  if (need > 0 && (!workspace || have < need)) return fail(nullptr, CDSL_EINVAL, "workspace too small");
+  if (!aligned16(workspace)) return fail(nullptr, CDSL_EINVAL, "the workspace must be 16-byte aligned");
+  return CDSL_OK;
+}
+
 int launched(hipError_t e) {
   return e == hipSuccess ? CDSL_OK : fail(nullptr, CDSL_EDEVICE, hipGetErrorString(e));
 }
@@ -2070,6 +2104,94 @@ int cdsl_op_kvq_keep(const cdsl_kvq* cache, const int32_t* lens, const int32_t* 
     if ((long long)cache->n_layers * cache->n_kv_heads > kMaxGroups) return fail(nullptr, CDSL_ERANGE, "too many heads");
     return launched(kvq_keep_launch(kvq_view(cache, 0), cache->n_layers, kvq_layer_bytes(cache), lens, path, n_path, n,
                                     new_lens, (hipStream_t)stream));
+  });
+}
+
+size_t cdsl_op_pages_workspace(int32_t batch, int32_t table_stride, int32_t pages, int32_t max_count) {
+  if (batch < 0 || batch > 65535 || table_stride <= 0 || table_stride >= (1 << 26) || pages <= 0 || pages > (1 << 30) ||
+      max_count < 0 || !pages_entries_fit(batch, max_count))
+    return 0;
+  const long long fork = batch > kForkRows ? (long long)batch * table_stride : 0;
+  return 4 * (size_t)std::max({fork, reserve_space(batch, pages, max_count).ints, compact_space(pages).ints});
+}
+
+int cdsl_op_pages_fork(const cdsl_kvq* cache, int32_t* table, int32_t* refs, const int32_t* parents, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    int rc = pages_check(cache, table, refs);
+    if (rc != CDSL_OK) return rc;
+    if (cache->batch == 0) return CDSL_OK;
+    if (!parents) return fail(nullptr, CDSL_EINVAL, "null argument");
+    if (!apart(cache, table, refs, parents, cache->batch))
+      return fail(nullptr, CDSL_EINVAL, "parents must not overlap table or refs");
+    const size_t need = cache->batch > kForkRows ? 4 * (size_t)cache->batch * cache->table_stride : 0;
+    rc = workspace_check(workspace, workspace_bytes, need);
+    if (rc != CDSL_OK) return rc;
+    return launched(pages_fork_launch(pages_args(cache, table, refs), parents, (int*)workspace, (hipStream_t)stream));
+  });
+}
+
+int cdsl_op_pages_reserve(const cdsl_kvq* cache, int32_t* table, int32_t* refs, const int32_t* lens, const int32_t* count,
+                          int32_t max_count, int32_t* got, void* workspace, size_t workspace_bytes, void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    int rc = pages_check(cache, table, refs);
+    if (rc != CDSL_OK) return rc;
+    if (max_count < 0) return fail(nullptr, CDSL_EINVAL, "bad token count");
+    if (cache->batch == 0) return CDSL_OK;
+    if (!lens || !count || !got) return fail(nullptr, CDSL_EINVAL, "null argument");
+    const int64_t B = cache->batch;
+    if (!apart(cache, table, refs, lens, B) || !apart(cache, table, refs, count, B) || !apart(cache, table, refs, got, B) ||
+        overlap(got, B, lens, B) || overlap(got, B, count, B))
+      return fail(nullptr, CDSL_EINVAL, "lens, count and got must not overlap table or refs, nor got the others");
+    if (!pages_entries_fit(cache->batch, max_count)) return fail(nullptr, CDSL_ERANGE, "too many pages at once");
+    rc = workspace_check(workspace, workspace_bytes, 4 * (size_t)reserve_space(cache->batch, cache->pages, max_count).ints);
+    if (rc != CDSL_OK) return rc;
+    return launched(pages_reserve_launch(pages_args(cache, table, refs), lens, count, max_count, got, (int*)workspace,
+                                         (hipStream_t)stream));
+  });
+}
+
+int cdsl_op_pages_free(const cdsl_kvq* cache, int32_t* table, int32_t* refs, const int32_t* lens, void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    const int rc = pages_check(cache, table, refs);
+    if (rc != CDSL_OK) return rc;
+    if (cache->batch == 0) return CDSL_OK;
+    if (!lens) return fail(nullptr, CDSL_EINVAL, "null argument");
+    if (!apart(cache, table, refs, lens, cache->batch))
+      return fail(nullptr, CDSL_EINVAL, "lens must not overlap table or refs");
+    return launched(pages_free_launch(pages_args(cache, table, refs), lens, (hipStream_t)stream));
+  });
+}
+
+int cdsl_op_pages_compact(const cdsl_kvq* cache, int32_t* table, int32_t* refs, int32_t* used, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    int rc = pages_check(cache, table, refs);
+    if (rc != CDSL_OK) return rc;
+    if (!refs || !used) return fail(nullptr, CDSL_EINVAL, "null argument");
+    if (!apart(cache, table, refs, used, 1)) return fail(nullptr, CDSL_EINVAL, "used must not overlap table or refs");
+    rc = workspace_check(workspace, workspace_bytes, 4 * (size_t)compact_space(cache->pages).ints);
+    if (rc != CDSL_OK) return rc;
+    return launched(pages_compact_launch(pages_args(cache, table, refs), used, (int*)workspace, (hipStream_t)stream));
+  });
+}
+
+int cdsl_op_pages_copy(const cdsl_kvq* from, const int32_t* src, const cdsl_kvq* to, const int32_t* dst, int32_t n,
+                       void* stream) {
+  return guarded(nullptr, [&]() -> int {
+    for (const cdsl_kvq* c : {from, to}) {
+      const int rc = kvq_check(c);
+      if (rc != CDSL_OK) return rc;
+      if (kvq_layer_bytes(c) / c->pages >> 34) return fail(nullptr, CDSL_ERANGE, "pages of 2^34 bytes or more");
+    }
+    if (n < 0) return fail(nullptr, CDSL_EINVAL, "bad page count");
+    if (from->n_layers != to->n_layers || from->n_kv_heads != to->n_kv_heads || from->head_dim != to->head_dim ||
+        from->format != to->format)
+      return fail(nullptr, CDSL_EINVAL, "the caches' layers, heads or formats differ");
+    if (n == 0) return CDSL_OK;
+    if (!src || !dst) return fail(nullptr, CDSL_EINVAL, "null argument");
+    return launched(pages_copy_launch(pages_args(from, nullptr, nullptr), src, (uint8_t*)to->pool, to->pages,
+                                      kvq_layer_bytes(to), dst, n, (hipStream_t)stream));
   });
 }
 
