@@ -30,10 +30,10 @@ CDSL_KVQ_HD PagesRun pages_run(int len, int count, int T, int P) {
 
 // Workspace of a reserve in ints: [pages] reservers, first reserver and last need
 // of each shared page, a state per entry of the runs, the free pages that are
-// handed out, and the copies.
+// handed out, the copies, and where each prompt's entries start.
 struct ReserveSpace {
-  long long entries;        // B * pages of a run
-  long long leave, first, last, need, free_ids, src, dst, jobs, ints;
+  long long entries;        // B * pages of a run: at most
+  long long leave, first, last, need, free_ids, src, dst, jobs, starts, ints;
 };
 CDSL_KVQ_HD ReserveSpace reserve_space(int B, int pages, int T) {
   ReserveSpace s;
@@ -47,7 +47,8 @@ CDSL_KVQ_HD ReserveSpace reserve_space(int B, int pages, int T) {
   s.src = s.free_ids + handed;
   s.dst = s.src + B;
   s.jobs = s.dst + B;
-  s.ints = s.jobs + 1;
+  s.starts = s.jobs + 1;
+  s.ints = s.starts + B + 1;
   return s;
 }
 

@@ -6,6 +6,7 @@
 // in which workgroups run: counts change by atomic additions, and which page goes
 // where follows from prefix sums over the pages and over the entries.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "pages.h"
@@ -91,168 +92,252 @@ __device__ __forceinline__ int wave_before(int v) {
 
 constexpr int kPlanThreads = 1024;
 
-// The sum over the threads before this one; total: over all.  sums: [16] in LDS,
-// of which two take turns, so that one barrier is enough.
-__device__ __forceinline__ int block_before(int v, int (*sums)[16], int& turn, int& total) {
+// The sums over the threads before this one, and over all; sums: in LDS, of which
+// two take turns, so that one barrier is enough.
+struct Sums {
+  int v[2][2][16];
+};
+template <int N>
+__device__ __forceinline__ void block_before(const int (&v)[N], Sums& sums, int& turn, int (&before)[N], int (&total)[N]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int before = wave_before(v);
-  if (lane == 63) sums[turn][wave] = before + v;
-  __syncthreads();
-  int at = before;
-  total = 0;
 #pragma unroll
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    const int s = sums[turn][w];
-    at += w < wave ? s : 0;
-    total += s;
+  for (int n = 0; n < N; ++n) {
+    before[n] = wave_before(v[n]);
+    if (lane == 63) sums.v[turn][n][wave] = before[n] + v[n];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    total[n] = 0;
+#pragma unroll
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+      const int s = sums.v[turn][n][w];
+      before[n] += w < wave ? s : 0;
+      total[n] += s;
+    }
   }
   turn ^= 1;
-  return at;
 }
 
-// What other threads of the workgroup wrote is there after this.
-__device__ __forceinline__ void block_fence() {
-  __threadfence();
-  __syncthreads();
+// Atomics and loads among the threads of one workgroup, which is all that works on
+// these arrays: no fence of the whole chip (four of them took 12 of 22 us).
+__device__ __forceinline__ int here_load(const int* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
-__device__ __forceinline__ int read_now(const int* p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ void here_store(int* p, int v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+__device__ __forceinline__ void here_add(int* p, int v) {
+  __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+__device__ __forceinline__ void here_min(int* p, int v) {
+  __hip_atomic_fetch_min(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+__device__ __forceinline__ void here_max(int* p, int v) {
+  __hip_atomic_fetch_max(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
+// Which of eight pages from p on are free (USED: used).
+template <bool USED>
+__device__ __forceinline__ unsigned page_mask(const PagesArgs& a, int p) {
+  unsigned mask = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = p + k < a.pages ? a.refs[p + k] : USED ? 0 : 1;
+    mask |= (USED ? r > 0 : r == 0) ? 1u << k : 0u;
+  }
+  return mask;
 }
 
 // States of an entry that needs no page (one that does: its number).
 constexpr int kFine = -1, kKeeps = -2;
+constexpr int kPlanPer = 8, kPlanChunk = kPlanThreads * kPlanPer;   // entries of a thread, of the workgroup at a time
 
 // The plan of a reserve, by one workgroup: pages and entries are few (4 bytes for
-// a page's megabyte), and every step waits for all of the one before.
+// a page's megabyte), and every step waits for all of the one before, so that what
+// bounds it is a chain of loads and barriers: 8 us for 64 prompts.  Entries are
+// those that the runs reach, in the order of the prompts, eight a thread; up to
+// kPlanChunk of them stay in registers, more are loaded again for every step (256
+// prompts of up to 65 pages each, of which they reach 3,000 entries: 12 us; with
+// all 16,640 taken as entries 55).
 __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(PagesArgs a, const int* lens, const int* count, int T, int* got,
                                                                int* ws) {
-  constexpr int PER = 8;                    // entries of a thread at a time
-  constexpr int CH = kPlanThreads * PER;
-  __shared__ int sums[2][16];
+  constexpr int PER = kPlanPer, CH = kPlanChunk, NEAR = 2048;
+  __shared__ Sums sums;
   __shared__ int n_jobs;
+  __shared__ int near_ids[CH];              // the first free pages
+  __shared__ int near_starts[NEAR + 1], near_lens[NEAR];
   int turn = 0;
   const ReserveSpace at = reserve_space(a.B, a.pages, T);
-  const int M = kvq_run_pages(T), E = (int)at.entries, tid = threadIdx.x;
+  const int tid = threadIdx.x;
   int *leave = ws + at.leave, *first = ws + at.first, *last = ws + at.last, *need = ws + at.need;
   int *free_ids = ws + at.free_ids, *src = ws + at.src, *dst = ws + at.dst;
+  const unsigned near = page_mask<false>(a, tid * PER);
+
+  // where each prompt's entries start
+  const bool few = a.B <= NEAR;
+  int* starts = few ? near_starts : ws + at.starts;
+  int E = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    int v[1] = {0}, before[1], total[1];
+    if (b < a.B) {
+      const int len = max(lens[b], 0);
+      const PagesRun r = pages_run(len, count[b], T, a.P);
+      got[b] = r.fit;
+      v[0] = r.end - r.first;
+      if (few) near_lens[b] = len;
+    }
+    block_before<1>(v, sums, turn, before, total);
+    if (b < a.B) starts[b] = E + before[0];
+    E += total[0];
+  }
+  if (tid == 0) {
+    starts[a.B] = E;
+    n_jobs = 0;
+  }
+  __syncthreads();
 
   struct Entry {
-    int b, i, id, refs, len;
-    bool in, held, shared;
+    int b, i, id, refs;                      // refs: -1 past the last entry
+    bool tokens;                             // the prompt has tokens on it
   };
-  auto entry = [&](int e) __attribute__((always_inline)) {
-    Entry x{};
-    if (e >= E) return x;
-    x.b = e / M;
-    x.len = max(lens[x.b], 0);
-    const PagesRun r = pages_run(x.len, count[x.b], T, a.P);
-    x.i = r.first + e % M;
-    x.in = x.i < r.end;
-    if (!x.in) return x;
-    x.id = a.table[(long long)x.b * a.P + x.i];
-    x.held = is_page(x.id, a.pages);
-    x.refs = x.held ? a.refs[x.id] : 0;
-    x.shared = x.refs > 1;
-    return x;
-  };
-
-  // which prompts leave a shared page in this call
-  if (tid == 0) n_jobs = 0;
-  for (int b = tid; b < a.B; b += kPlanThreads) got[b] = pages_run(lens[b], count[b], T, a.P).fit;
-  bool any = false;
-  for (int e = tid; e < E; e += kPlanThreads) {
-    const Entry x = entry(e);
-    if (x.shared) {
-      leave[x.id] = 0;
-      first[x.id] = 0x7fffffff;
-      last[x.id] = -1;
-      any = true;
-    }
-  }
-  any = __syncthreads_or(any);
-  if (any) {
-    block_fence();
-    for (int e = tid; e < E; e += kPlanThreads) {
-      const Entry x = entry(e);
-      if (x.shared) {
-        atomicAdd(&leave[x.id], 1);
-        atomicMin(&first[x.id], e);
+  // this thread's entries from e on
+  auto load = [&](int e, Entry (&x)[PER]) __attribute__((always_inline)) {
+    int low = 0, high = a.B;                 // the last prompt that starts at or before e
+    if (e < E)
+      while (high - low > 1) {
+        const int mid = (low + high) / 2;
+        if (starts[mid] <= e) low = mid;
+        else high = mid;
       }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      x[k] = {0, 0, -1, -1, false};
+      if (e + k >= E) continue;
+      while (starts[low + 1] <= e + k) ++low;
+      const int len = few ? near_lens[low] : max(lens[low], 0);
+      x[k].b = low;
+      x[k].i = len / kPage + (e + k - starts[low]);
+      x[k].tokens = (long long)x[k].i * kPage < len;
+      x[k].id = a.table[(long long)low * a.P + x[k].i];
+      if (!is_page(x[k].id, a.pages)) x[k].id = -1;
     }
-    block_fence();
-  }
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (e + k < E) x[k].refs = x[k].id >= 0 ? a.refs[x[k].id] : 0;
+  };
+  auto classify = [&](const Entry& x, int e, int& n) __attribute__((always_inline)) {
+    if (x.refs < 0 || x.refs == 1 || (x.refs == 0 && x.id >= 0)) return kFine;
+    if (x.refs > 1 && here_load(&leave[x.id]) == x.refs && here_load(&first[x.id]) == e) return kKeeps;
+    return n++;
+  };
 
-  // the entries that need a page, numbered
-  int needed = 0;
-  for (int e0 = 0; e0 < E; e0 += CH) {
-    int state[PER], n = 0;
+  auto plan = [&](auto registers) __attribute__((always_inline)) {
+    constexpr bool ONE = decltype(registers)::value;
     Entry x[PER];
+    int state[PER];
+    if constexpr (ONE) load(tid * PER, x);
+    // f(its first number) for this thread's entries, x
+    auto each = [&](auto f) __attribute__((always_inline)) {
+      if constexpr (ONE) f(tid * PER);
+      else
+        for (int e0 = 0; e0 < E; e0 += CH) {
+          load(e0 + tid * PER, x);
+          f(e0 + tid * PER);
+        }
+    };
+
+    // which prompts leave a shared page in this call
+    int any = 0;
+    each([&](int) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int e = e0 + tid * PER + k;
-      x[k] = entry(e);
-      state[k] = kFine;
-      if (x[k].shared && read_now(&leave[x[k].id]) == x[k].refs && read_now(&first[x[k].id]) == e) state[k] = kKeeps;
-      else if (x[k].in && (!x[k].held || x[k].shared)) state[k] = n++;
-    }
-    int total;
-    const int base = needed + block_before(n, sums, turn, total);
-    needed += total;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int e = e0 + tid * PER + k;
-      if (e >= E) break;
-      if (state[k] >= 0) {
-        state[k] += base;
-        if (x[k].shared) atomicMax(&last[x[k].id], state[k]);
+      for (int k = 0; k < PER; ++k) {
+        if (x[k].refs <= 1) continue;
+        any = 1;
+        here_store(&leave[x[k].id], 0);
+        here_store(&first[x[k].id], 0x7fffffff);
+        here_store(&last[x[k].id], -1);
       }
-      need[e] = state[k];
-    }
-  }
-
-  // the lowest free pages, as many as are needed
-  int found = 0;
-  for (int p0 = 0; p0 < a.pages && found < needed; p0 += CH) {
-    unsigned mask = 0;
+    });
+    if (__syncthreads_or(any)) {
+      each([&](int e) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int p = p0 + tid * PER + k;
-      if (p < a.pages && a.refs[p] == 0) mask |= 1u << k;
+        for (int k = 0; k < PER; ++k) {
+          if (x[k].refs <= 1) continue;
+          here_add(&leave[x[k].id], 1);
+          here_min(&first[x[k].id], e + k);
+        }
+      });
+      __syncthreads();
     }
-    int total;
-    int n = found + block_before(__popc(mask), sums, turn, total);
-    found += total;
-    for (; mask && n < needed; mask &= mask - 1) free_ids[n++] = p0 + tid * PER + __builtin_ctz(mask);
-  }
-  block_fence();
 
-  // each gets its page
-  for (int e0 = 0; e0 < E; e0 += CH)
-    for (int k = 0; k < PER; ++k) {
-      const int e = e0 + tid * PER + k;
-      if (e >= E) break;
-      const int s = need[e];   // written by this thread
-      if (s == kFine) continue;
-      const int b = e / M, len = max(lens[b], 0), i = len / kPage + e % M;
-      int* slot = &a.table[(long long)b * a.P + i];
-      const int old = *slot;
-      const bool ok = s == kKeeps ? read_now(&last[old]) < found : s < found;
-      if (!ok) {
-        atomicMin(&got[b], max(0, (int)max((long long)i * kPage - len, 0ll)));
-      } else if (s >= 0) {
-        const int now = free_ids[s];
-        *slot = now;
+    // the entries that need a page, numbered, and the lowest pages that are free
+    int needed = 0, found = 0;
+    auto search = [&](int before, unsigned mask, int p) __attribute__((always_inline)) {
+      for (; mask; mask &= mask - 1, ++before) {
+        const int id = p + __builtin_ctz(mask);
+        if (before < CH) near_ids[before] = id;
+        else if (before < needed) free_ids[before] = id;
+      }
+    };
+    each([&](int e) __attribute__((always_inline)) {
+      int v[2] = {0, ONE ? (int)__popc(near) : 0}, before[2], total[2];
+#pragma unroll
+      for (int k = 0; k < PER; ++k) state[k] = classify(x[k], e + k, v[0]);
+      block_before<2>(v, sums, turn, before, total);
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        if (state[k] >= 0) {
+          state[k] += needed + before[0];
+          if (x[k].refs > 1) here_max(&last[x[k].id], state[k]);
+        }
+        if (!ONE && e + k < E) need[e + k] = state[k];
+      }
+      needed += total[0];
+      if constexpr (ONE) {
+        found = total[1];
+        if (needed) search(before[1], near, tid * PER);
+      }
+    });
+    for (int p0 = ONE ? CH : 0; p0 < a.pages && found < needed; p0 += CH) {
+      const unsigned mask = p0 == 0 ? near : page_mask<false>(a, p0 + tid * PER);
+      int v[1] = {(int)__popc(mask)}, before[1], total[1];
+      block_before<1>(v, sums, turn, before, total);
+      search(found + before[0], mask, p0 + tid * PER);
+      found += total[0];
+    }
+    __syncthreads();
+
+    // each gets its page
+    each([&](int e) __attribute__((always_inline)) {
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        if (x[k].refs < 0) continue;
+        const int s = ONE ? state[k] : need[e + k];   // written by this thread
+        if (s == kFine) continue;
+        const bool ok = s == kKeeps ? here_load(&last[x[k].id]) < found : s < found;
+        if (!ok) {
+          const long long len = few ? near_lens[x[k].b] : max(lens[x[k].b], 0);
+          here_min(&got[x[k].b], (int)max((long long)x[k].i * kPage - len, 0ll));
+          continue;
+        }
+        if (s == kKeeps) continue;
+        const int now = s < CH ? near_ids[s] : free_ids[s];
+        a.table[(long long)x[k].b * a.P + x[k].i] = now;
         a.refs[now] = 1;
-        if (is_page(old, a.pages)) {
-          atomicSub(&a.refs[old], 1);
-          if ((long long)i * kPage < len) {   // it holds tokens of the prompt
-            const int j = atomicAdd(&n_jobs, 1);
-            src[j] = old;
-            dst[j] = now;
-          }
+        if (x[k].id < 0) continue;
+        here_add(&a.refs[x[k].id], -1);
+        if (x[k].tokens) {
+          const int j = atomicAdd(&n_jobs, 1);
+          src[j] = x[k].id;
+          dst[j] = now;
         }
       }
-    }
+    });
+  };
+  if (E <= CH) plan(std::true_type{});
+  else plan(std::false_type{});
   __syncthreads();
   if (tid == 0) ws[at.jobs] = n_jobs;
 }
@@ -261,29 +346,27 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(PagesArgs a, cons
 // below that is free and below U takes what the k-th from above that is used and not
 // below U holds.
 __global__ __launch_bounds__(kPlanThreads) void compact_kernel(PagesArgs a, int* used, int* ws) {
-  constexpr int PER = 8, CH = kPlanThreads * PER;
-  __shared__ int sums[2][16];
+  constexpr int PER = kPlanPer, CH = kPlanChunk;
+  __shared__ Sums sums;
   int turn = 0;
   const CompactSpace at = compact_space(a.pages);
   const int tid = threadIdx.x;
-  int n = 0, U;
-  for (int p = tid; p < a.pages; p += kPlanThreads) n += a.refs[p] > 0 ? 1 : 0;
-  block_before(n, sums, turn, U);
+  const unsigned near = page_mask<true>(a, tid * PER);
+  int v[1] = {(int)__popc(near)}, below[1], total[1];
+  for (int p0 = CH; p0 < a.pages; p0 += CH) v[0] += __popc(page_mask<true>(a, p0 + tid * PER));
+  block_before<1>(v, sums, turn, below, total);
+  const int U = total[0];
   if (tid == 0) {
     *used = U;
     if (U == a.pages) ws[at.moves] = 0;
   }
   int before = 0;   // used pages below
   for (int p0 = 0; p0 < a.pages; p0 += CH) {
-    unsigned mask = 0;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int p = p0 + tid * PER + k;
-      if (p < a.pages && a.refs[p] > 0) mask |= 1u << k;
-    }
-    int total;
-    int u = before + block_before(__popc(mask), sums, turn, total);
-    before += total;
+    const unsigned mask = p0 == 0 ? near : page_mask<true>(a, p0 + tid * PER);
+    v[0] = __popc(mask);
+    block_before<1>(v, sums, turn, below, total);
+    int u = before + below[0];
+    before += total[0];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int p = p0 + tid * PER + k;
@@ -394,10 +477,10 @@ hipError_t pages_free_launch(const PagesArgs& a, const int* lens, hipStream_t st
 hipError_t pages_reserve_launch(const PagesArgs& a, const int* lens, const int* count, int T, int* got, int* workspace,
                                 hipStream_t st) {
   if (a.B == 0) return hipSuccess;
+  const ReserveSpace at = reserve_space(a.B, a.pages, T);
   reserve_kernel<<<1, kPlanThreads, 0, st>>>(a, lens, count, T, got, workspace);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || T == 0) return e;
-  const ReserveSpace at = reserve_space(a.B, a.pages, T);
   // a prompt copies one page at most: the one that its tokens end in
   const CopyArgs c = copy_within(a, workspace + at.src, workspace + at.dst, workspace + at.jobs);
   const long long items = (long long)a.B * a.n_layers * c.pieces.count;

@@ -42,9 +42,9 @@ static void spaces() {
       for (int T : {0, 1, 32, 5000}) {
         const ReserveSpace s = reserve_space(B, pages, T);
         CHECK(s.entries == (long long)B * kvq_run_pages(T));
-        const long long at[] = {s.leave, s.first, s.last, s.need, s.free_ids, s.src, s.dst, s.jobs, s.ints};
-        const long long n[] = {pages, pages, pages, s.entries, std::min<long long>(s.entries, pages), B, B, 1};
-        for (int i = 0; i < 8; ++i) CHECK(at[i] + n[i] == at[i + 1]);
+        const long long at[] = {s.leave, s.first, s.last, s.need, s.free_ids, s.src, s.dst, s.jobs, s.starts, s.ints};
+        const long long n[] = {pages, pages, pages, s.entries, std::min<long long>(s.entries, pages), B, B, 1, B + 1};
+        for (int i = 0; i < 9; ++i) CHECK(at[i] + n[i] == at[i + 1]);
       }
   for (int pages : {1, 2, 3, 1001, 1 << 30}) {
     const CompactSpace s = compact_space(pages);
