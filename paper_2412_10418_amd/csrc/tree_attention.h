@@ -199,6 +199,7 @@ __device__ __forceinline__ TreeParts tree_parts(const TreeAttnArgs& a, int lane)
 // tiles of a (prompt, KV head).
 struct TreeSpan {
   int b, kvh, slot, parts, nrows, row0, L, nb, node0, node1, beg, end;
+  int turn;    // counts the workgroups of a row group on an XCD
   bool over, none;
 };
 
@@ -218,6 +219,7 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeAttnArgs& a, int tiles) 
     rg = x % NR;
   }
   const int lane = threadIdx.x & 63, B = a.c.B;
+  t.turn = chunk >> 3;
   t.slot = chunk / a.c.Hkv;
   t.kvh = chunk % a.c.Hkv;
   t.parts = a.slots / B;

@@ -97,18 +97,65 @@ __device__ __forceinline__ void fp4_hold(unsigned& w, unsigned& s, unsigned m) {
   s &= m & ~(none | (none - (none >> 7)));
 }
 
+// The largest of N values, a NaN if one is (an instruction takes three; fmaxf would
+// make each value canonical first).
+template <int N>
+__device__ __forceinline__ float max_of(const float (&x)[N]) {
+  float m = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = __builtin_elementwise_maximum(m, x[i]);
+  return m;
+}
+
 __device__ __forceinline__ unsigned held_mask(int held) {
   return held >= 32 ? ~0u : held <= 0 ? 0u : (1u << held) - 1u;
 }
 
-// q as bf16 planes of eight bits, by truncation (of bf16: itself), with the sign
-// of the softmax scale; zeros for a scale of 0.
+// Three bf16 planes of eight bits of each probability, by truncation.  The product
+// of a pair of planes with (-1, 0) or (0, -1) takes one of them from its value, an
+// exact difference in one instruction for two.  (The pairs are kept from the
+// compiler: it writes (-1, 0) as the constant -1.0, which the instruction reads as
+// (0, -1).)
+__device__ __forceinline__ void fp4_p_planes(float (&w)[8], bf16x8 (&pf)[3]) {
+  union {
+    unsigned u[4];
+    bf16x2v p[4];
+    bf16x8 v;
+  } o;
+  union {
+    unsigned u;
+    bf16x2v p;
+  } lower, upper;
+  lower.u = 0xbf80u;
+  upper.u = 0xbf800000u;
+  asm("" : "+s"(lower.u), "+s"(upper.u));
+#pragma unroll
+  for (int pl = 0; pl < 3; ++pl) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o.u[e] = __builtin_amdgcn_perm(__float_as_uint(w[2 * e + 1]), __float_as_uint(w[2 * e]), 0x07060302);
+    pf[pl] = o.v;
+    if (pl == 2) break;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[2 * e] = __builtin_amdgcn_fdot2_f32_bf16(o.p[e], lower.p, w[2 * e], false);
+      w[2 * e + 1] = __builtin_amdgcn_fdot2_f32_bf16(o.p[e], upper.p, w[2 * e + 1], false);
+    }
+  }
+}
+template <int PP>
+__device__ __forceinline__ void fp4_p_planes(float (&w)[8], bf16x8 (&pf)[PP]) {
+  p_planes<PP>(w, pf);
+}
+
+// q as bf16 planes, with the sign of the softmax scale (zeros for a scale of 0): of
+// fp32 three of eight bits, by truncation, of bf16 itself.
 template <typename QT, int QP>
-__device__ __forceinline__ void fp4_q8(const QT* p, float sign, bf16x8 (&q)[QP]) {
+__device__ __forceinline__ void fp4_q8(const QT* p, float scale, bf16x8 (&q)[QP]) {
   float x[8];
   load_q8<QT>(p, x);
+  const float by = scale < 0.f ? -1.f : scale > 0.f ? 1.f : 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] *= sign;
+  for (int e = 0; e < 8; ++e) x[e] *= by;
   if constexpr (QP == 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) q[0][e] = (bf16)x[e];
@@ -116,10 +163,42 @@ __device__ __forceinline__ void fp4_q8(const QT* p, float sign, bf16x8 (&q)[QP])
     p_planes<QP>(x, q);
   }
 }
-__device__ __forceinline__ float sign_of(float scale) { return scale < 0.f ? -1.f : scale > 0.f ? 1.f : 0.f; }
-// What a score counts in log2 units.  It meets the -inf of hidden slots, so it is
-// above 0 (scores are 0 where the scale is).
-__device__ __forceinline__ float score_unit(float scale) { return fmaxf(fabsf(scale), 0x1p-126f); }
+
+// A row's running maximum and sum.  The maximum may lag by kLazy, so that O is
+// rescaled rarely; O / l does not depend on it.
+struct Fp4Softmax {
+  float rm;            // log2 units of a score; it meets the -inf of hidden slots, so it is above 0
+  float m, l;          // running maximum (log2 units; -inf before the first visible key), this lane's part of the sum
+  __device__ __forceinline__ void init(float scale, bool over) {
+    rm = fmaxf(fabsf(scale), 0x1p-126f);
+    m = -INFINITY;
+    l = over ? __uint_as_float(0x7fc00000u) : 0.f;
+  }
+  // Raises the maximum to a page's, the row's largest score `most`, where it lags;
+  // scale(c): O *= c.
+  template <typename F>
+  __device__ __forceinline__ void raise(float most, F scale) {
+    most *= rm;
+    const bool up = most > m + kLazy;   // true for the first visible key
+    if (__ballot(up)) {
+      const float to = up ? most : m;
+      const float corr = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      l *= corr;
+      scale(corr);
+      m = to;
+    }
+  }
+  // Scores to probabilities.
+  template <int N>
+  __device__ __forceinline__ void exps(float (&s)[N]) {
+    const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], rm, -mu));
+      l += s[e];
+    }
+  }
+};
 
 // One tile of 16 rows in a wave: lane (row lr = lane % 16, group lg = lane / 16).
 template <int HD, typename QT, int PLANES>
@@ -128,9 +207,8 @@ struct Fp4Tile {
   static constexpr int QP = sizeof(QT) == 4 ? 3 : 1;   // planes of q
   static constexpr int PP = PLANES;                    // and of p
   bf16x8 q[S][QP];
-  float rm;              // what a score counts in log2 units
   f32x4 acc[DT];         // tiles (s, even) and (s, odd): dims 32 s + 8 lg + 2 e (+ 1) of row lr
-  float m, l;            // running maximum (log2 units) and this lane's part of the sum
+  Fp4Softmax sm;
   int node, head;
   bool valid;
 
@@ -140,50 +218,33 @@ struct Fp4Tile {
     node = r / a.G;
     head = t.kvh * a.G + r % a.G;
     const QT* qp = (const QT*)a.q + t.b * a.qsb + node * a.qst + (long long)head * HD + 8 * lg;
-    const float sign = sign_of(a.scale_log2);
-    rm = score_unit(a.scale_log2);
 #pragma unroll
-    for (int s = 0; s < S; ++s) fp4_q8<QT, QP>(qp + 32 * s, sign, q[s]);
+    for (int s = 0; s < S; ++s) fp4_q8<QT, QP>(qp + 32 * s, a.scale_log2, q[s]);
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    m = -INFINITY;
-    l = t.over ? __uint_as_float(0x7fc00000u) : 0.f;
+    sm.init(a.scale_log2, t.over);
   }
-
   // Probabilities of a page as planes, from its scores (slots 4 lg + e and 16 + 4
-  // lg + e).  The running maximum may lag by kLazy, so that O is rescaled rarely.
-  __device__ __forceinline__ void softmax(const float (&s)[8], bf16x8 (&pf)[PP]) {
-    float mt = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    mt = groups_max(mt) * rm;
-    const bool raise = mt > m + kLazy;   // true for the first visible key
-    if (__ballot(raise)) {
-      const float to = raise ? mt : m;
-      const float corr = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
-      l *= corr;
+  // lg + e).
+  __device__ __forceinline__ void softmax(float (&s)[8], bf16x8 (&pf)[PP]) {
+    sm.raise(groups_max(max_of(s)), [&](float c) __attribute__((always_inline)) {
 #pragma unroll
-      for (int d = 0; d < DT; ++d) acc[d] *= corr;
-      m = to;
-    }
-    const float mu = m == -INFINITY ? 0.f : m;
-    float p[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(fmaf(s[e], rm, -mu));
-      l += p[e];
-    }
-    p_planes<PP>(p, pf);
+      for (int d = 0; d < DT; ++d) acc[d] *= c;
+    });
+    sm.exps(s);
+    fp4_p_planes(s, pf);
   }
 
   __device__ __forceinline__ void finish() {
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
+    sm.l += __shfl_xor(sm.l, 16, 64);
+    sm.l += __shfl_xor(sm.l, 32, 64);
   }
 
   // The result, or this split's part of it.
   __device__ __forceinline__ void store(const TreeAttnArgs& a, const TreeSpan& t, int lg) {
     if (!valid) return;
     const bool whole = t.parts == 1;
-    const float inv = whole ? 1.f / l : 1.f;
+    const float inv = whole ? 1.f / sm.l : 1.f;
     const long long row = ((long long)t.b * a.n + node) * a.H + head;
     const long long prow = ((long long)t.slot * a.n + node) * a.H + head;
 #pragma unroll
@@ -200,8 +261,8 @@ struct Fp4Tile {
       }
     }
     if (!whole && lg == 0) {
-      a.part_ml[prow * 2] = m;
-      a.part_ml[prow * 2 + 1] = l;
+      a.part_ml[prow * 2] = sm.m;
+      a.part_ml[prow * 2 + 1] = sm.l;
     }
   }
 };
@@ -220,9 +281,11 @@ __device__ __forceinline__ void fp4_score_step(const Row (&row)[RPW], int s, con
 }
 
 // Planes of p of every row tile of a wave, from a page's scores.  MASKED: the
-// page holds nodes.  none: this lane's slots whose values are NaN (bit e).
+// page holds nodes.  none: this lane's slots whose values are NaN (bit e).  bad: NaN
+// for a page that does not exist, which the sums of the rows that see a slot of it
+// take up; else 0.
 template <bool MASKED, typename Row, int RPW>
-__device__ __forceinline__ void fp4_softmax(Row (&row)[RPW], const f32x4 (&sc)[RPW][2], bool bad, unsigned none,
+__device__ __forceinline__ void fp4_softmax(Row (&row)[RPW], const f32x4 (&sc)[RPW][2], float bad, unsigned none,
                                             bool tree, int i0, int node0, const uint32_t* masks, int lg,
                                             bf16x8 (&pf)[RPW][Row::PP]) {
   const float nan = __uint_as_float(0x7fc00000u);
@@ -230,17 +293,21 @@ __device__ __forceinline__ void fp4_softmax(Row (&row)[RPW], const f32x4 (&sc)[R
   for (int r = 0; r < RPW; ++r) {
     float s[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = bad ? nan : sc[r][e >> 2][e & 3];
+    for (int e = 0; e < 8; ++e) s[e] = sc[r][e >> 2][e & 3];
     if constexpr (MASKED) {
       const unsigned vis = (tree ? slots_of_tree(i0, masks + (row[r].node - node0) * kTreeWords)
                                  : slots_of_chain(i0, row[r].node)) >> (4 * lg);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         s[e] = !(vis >> (e < 4 ? e : 12 + e) & 1u) ? -INFINITY : none >> e & 1u ? nan : s[e];
+      row[r].sm.l += vis & 0x000f000fu ? bad : 0.f;
+    } else {
+      row[r].sm.l += bad;
     }
     row[r].softmax(s, pf[r]);
   }
 }
+__device__ __forceinline__ float bad_page(bool bad) { return bad ? __uint_as_float(0x7fc00000u) : 0.f; }
 
 // This lane's slots whose value scales are 255, bit e (from the words of block 0).
 __device__ __forceinline__ unsigned fp4_none_bits(unsigned s0, unsigned s1) {
@@ -338,7 +405,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void f
         }
     }
     bf16x8 pf[RPW][Row::PP];
-    fp4_softmax<MASKED>(row, sc, now.bad, none, tree, page * kPage - t.L, t.node0, masks, lg, pf);
+    fp4_softmax<MASKED>(row, sc, bad_page(now.bad), none, tree, page * kPage - t.L, t.node0, masks, lg, pf);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int c = s / W, i = s % W * 2;
@@ -363,8 +430,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void f
 #pragma unroll
     for (int r = 0; r < RPW; ++r) {
       float* x = lds + ((kw - 1) * RPW + r) * SLOT;
-      x[lane] = row[r].m;
-      x[64 + lane] = row[r].l;
+      x[lane] = row[r].sm.m;
+      x[64 + lane] = row[r].sm.l;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -379,59 +446,90 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void f
     for (int k = 1; k < KW; ++k) {
       const float* x = lds + ((k - 1) * RPW + r) * SLOT;
       const float mq = x[lane], lq = x[64 + lane];
-      const float mn = fmaxf(row[r].m, mq);
-      const float s0 = row[r].m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(row[r].m - mn);
+      const float mn = fmaxf(row[r].sm.m, mq);
+      const float s0 = row[r].sm.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(row[r].sm.m - mn);
       const float s1 = mq == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mq - mn);
-      row[r].l = row[r].l * s0 + lq * s1;
+      row[r].sm.l = row[r].sm.l * s0 + lq * s1;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           row[r].acc[d][e] = row[r].acc[d][e] * s0 + x[(2 + 4 * d + e) * 64 + lane] * s1;
-      row[r].m = mn;
+      row[r].sm.m = mn;
     }
     row[r].store(a, t, lg);
   }
 }
 
-// Loads and expansion of a page for all waves of a workgroup: a piece of eight
-// bytes (a lane's codes of one block) a thread at a time, with the scales that go
-// with it.
+// Loads and expansion of a page by the four waves of a workgroup.  A piece is a
+// lane's eight bytes of codes of one block of 32 dims, keys (2 HD pieces) or values
+// (2 HD), with the scales that go with it; a wave takes 64 of one kind at a time.
 template <int HD>
 struct Fp4Pieces {
-  static constexpr int NT = 256, W = fp4_pair(HD);
-  static constexpr int N = 4 * HD;                 // keys' 2 HD, then values'
+  static constexpr int NT = 256, P = fp4_pair(HD);
+  static constexpr int N = 4 * HD;
   static constexpr int PER = (N + NT - 1) / NT;
   static constexpr int UNIT = fp4_unit_bytes(HD);
-  u32x2 codes[PER], scales[PER];                   // of keys: two bytes of scales in .x
-  bool bad;
+  struct Raw {
+    u32x2 codes[PER], scales[PER];   // of keys: two bytes of scales in .x
+    bool bad;
+  };
+  unsigned at[PER], scale_at[PER];   // offsets in a unit
+  int wave;
 
-  static __device__ __forceinline__ bool keys(int c) { return N >= 2 * NT ? c < PER / 2 : (int)threadIdx.x < 2 * HD; }
-  // block and lane of a piece
+  // Of piece c: whether there is one and its kind (uniform over a wave); its block and
+  // lane.
+  __device__ __forceinline__ bool any(int c) const { return NT * (c + 1) <= N || 64 * wave + NT * c < N; }
+  __device__ __forceinline__ bool keys(int c) const {
+    return NT * (c + 1) <= 2 * HD ? true : NT * c >= 2 * HD ? false : 64 * wave < 2 * HD;
+  }
   static __device__ __forceinline__ int piece(int c) { return ((int)threadIdx.x + NT * c) & (2 * HD - 1); }
-  static __device__ __forceinline__ int block(int j) { return W == 2 ? j / 128 * 2 + j % 2 : 0; }
-  static __device__ __forceinline__ int lane(int j) { return W == 2 ? j / 2 % 64 : j; }
+  static __device__ __forceinline__ int block(int c) { return P == 2 ? piece(c) / 128 * 2 + piece(c) % 2 : 0; }
+  static __device__ __forceinline__ int lane(int c) { return P == 2 ? piece(c) / 2 % 64 : piece(c); }
+  // Neighbouring threads have the same lane of two blocks, whose operands lie some
+  // multiple of all banks apart: of odd blocks, lanes trade places four apart.
+  static __device__ __forceinline__ int turned(int lane, int block) { return P == 2 ? lane ^ (block & 1) * 4 : lane; }
 
-  __device__ __forceinline__ void load(const uint8_t* u) {
+  __device__ __forceinline__ void init(int w) {
+    wave = w;
 #pragma unroll
     for (int c = 0; c < PER; ++c) {
-      const int i = threadIdx.x + NT * c;
-      if (N % NT != 0 && i >= N) continue;
-      codes[c] = *((const u32x2*)u + i);
-      const int j = piece(c), s = block(j), l = lane(j);
-      if (keys(c)) scales[c].x = *(const uint16_t*)(u + fp4_key_scale_at(HD, l % 16, 32 * s));
-      else scales[c] = *(const u32x2*)(u + fp4_value_scale_at(HD, l / 16 * 4, 32 * s));
+      const int s = block(c), l = lane(c);
+      at[c] = 8u * (threadIdx.x + NT * c);
+      scale_at[c] = keys(c) ? fp4_key_scale_at(HD, l % 16, 32 * s) : fp4_value_scale_at(HD, l / 16 * 4, 32 * s);
     }
+  }
+  __device__ __forceinline__ void load(Raw& r, const uint8_t* u) const {
+#pragma unroll
+    for (int c = 0; c < PER; ++c) {
+      if (!any(c)) continue;
+      r.codes[c] = *(const u32x2*)(u + at[c]);
+      if (keys(c)) r.scales[c].x = *(const uint16_t*)(u + scale_at[c]);
+      else r.scales[c] = *(const u32x2*)(u + scale_at[c]);
+    }
+  }
+  // Codes and scales of a value piece of a page with nodes, from whose slot `held` on
+  // there are none; gone: [slot], 1 where a value is NaN.
+  static __device__ __forceinline__ void hold(int c, u32x2& w, u32x2& e, uint8_t* gone, int held) {
+    const int x = lane(c) % 16, g = lane(c) / 16;
+    unsigned w0 = w.x, w1 = w.y, e0 = e.x, e1 = e.y;
+    if (block(c) == 0 && x < 8)   // one of the lanes that have these slots
+      gone[x / 4 * 16 + g * 4 + x % 4] = fp4_none(x < 4 ? e0 : e1) >> (8 * (x % 4) + 7) & 1u;
+    const unsigned hm = held_mask(held) >> (4 * g);
+    fp4_hold(w0, e0, hm);
+    fp4_hold(w1, e1, hm >> 16);
+    w = (u32x2){w0, w1};
+    e = (u32x2){e0, e1};
   }
 };
 
 // More rows.  Workgroup = (key split, prompt x KV head, group of a.wg_tiles row
 // tiles); wave w takes tile w.  A page is expanded once for all waves: its codes
 // come in two pages before they are needed and go to LDS as bf16 in operand order.
-template <int HD, typename QT, int EU>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EU))) void fp4_many_kernel(TreeAttnArgs a) {
+template <int HD, typename QT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) == 4 ? 3 : 4))) void fp4_many_kernel(TreeAttnArgs a) {
   using Row = Fp4Tile<HD, QT, sizeof(QT) == 4 ? 3 : 1>;
-  using In = Fp4Pieces<HD>;
+  using Pieces = Fp4Pieces<HD>;
   constexpr int NT = 256, W = 4;
   constexpr int S = Row::S, DT = Row::DT;
   constexpr int ROWS = 16 * W;
@@ -446,65 +544,55 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EU))) void 
   const TreeSpan t = tree_span(a, a.wg_tiles);
   if (t.none) return;   // uniform over the workgroup
   const int npages = t.end - t.beg;
-  const int wrow = t.row0 + 16 * wave;
+  const int wrow = t.row0 + 16 * ((wave + t.turn) % W);   // where tiles are missing, not always the same SIMD's
   const int wend = min(t.row0 + 16 * a.wg_tiles, t.nrows);
   const bool has_rows = wrow < wend;
 
   const int* table = a.c.table + (long long)t.b * a.c.table_stride + t.beg;
-  // Two pages in flight.  Loads past the last page repeat it: without a branch
-  // the compiler knows how many are outstanding, and waits for the older page
-  // alone.
-  In in[2];
+  // The next page's codes are in flight while one is computed.  (Loads past the last
+  // page repeat it.)
+  Pieces pieces;
+  pieces.init(wave);
+  typename Pieces::Raw in;
   int id_next = npages > 0 ? table[0] : 0;   // of the page that is loaded next: a scalar load, one step ahead
-  auto load = [&](int it, int slot) __attribute__((always_inline)) {
+  auto load = [&](int it) __attribute__((always_inline)) {
     const int id = id_next;
     id_next = table[min(it + 1, npages - 1)];
-    in[slot].bad = id < 0 || id >= a.c.pages;
-    in[slot].load(a.c.pool + ((long long)(in[slot].bad ? 0 : id) * a.c.Hkv + t.kvh) * In::UNIT);
+    in.bad = id < 0 || id >= a.c.pages;
+    pieces.load(in, a.c.pool + ((long long)(in.bad ? 0 : id) * a.c.Hkv + t.kvh) * Pieces::UNIT);
   };
-  bool page_bad[2] = {false, false};
+  float page_bad[2] = {0.f, 0.f};
   auto put = [&](int it, int buf) __attribute__((always_inline)) {
     const int page = t.beg + it;
-    page_bad[buf] = in[buf].bad;
+    page_bad[buf] = bad_page(in.bad);
     const bool nodes = (page + 1) * kPage > t.L;
 #pragma unroll
-    for (int c = 0; c < In::PER; ++c) {
-      if (In::N % NT != 0 && tid + NT * c >= In::N) continue;
-      const int j = In::piece(c), s = In::block(j), l = In::lane(j);
-      u32x2 w = in[buf].codes[c], e = in[buf].scales[c];
+    for (int c = 0; c < Pieces::PER; ++c) {
+      if (!pieces.any(c)) continue;
+      const int s = Pieces::block(c), l = Pieces::lane(c);
+      u32x2 w = in.codes[c], e = in.scales[c];
       union {
         bf16x8 b;
         u32x4 u;
       } x, y;
-      if (In::keys(c)) {
+      u32x4* at = &tile[buf][((pieces.keys(c) ? 0 : 2 * S) + 2 * s) * 64 + Pieces::turned(l, s)];
+      if (pieces.keys(c)) {
         x.b = fp4_key(w.x, fp4_scale_of(e.x, 0));
         y.b = fp4_key(w.y, fp4_scale_of(e.x, 1));
-        tile[buf][(2 * s) * 64 + l] = x.u;
-        tile[buf][(2 * s + 1) * 64 + l] = y.u;
       } else {
-        if (nodes) {
-          const unsigned hm = held_mask(in[buf].bad ? 0 : t.L + t.nb - page * kPage) >> (l / 16 * 4);
-          if (s == 0 && l % 16 < 8) {   // one of the lanes that have these slots
-            const int q = l % 16;
-            gone[buf][q / 4 * 16 + l / 16 * 4 + q % 4] = (q < 4 ? fp4_none(e.x) : fp4_none(e.y)) >> (8 * (q % 4) + 7) & 1u;
-          }
-          unsigned w0 = w.x, w1 = w.y, e0 = e.x, e1 = e.y;
-          fp4_hold(w0, e0, hm);
-          fp4_hold(w1, e1, hm >> 16);
-          w = (u32x2){w0, w1};
-          e = (u32x2){e0, e1};
-        }
+        if (nodes) Pieces::hold(c, w, e, gone[buf], in.bad ? 0 : t.L + t.nb - page * kPage);
         const unsigned wv[2] = {w.x, w.y}, ev[2] = {e.x, e.y};
         fp4_values(wv, ev, x.b, y.b);
-        tile[buf][(2 * S + 2 * s) * 64 + l] = x.u;
-        tile[buf][(2 * S + 2 * s + 1) * 64 + l] = y.u;
       }
+      at[0] = x.u;
+      at[64] = y.u;
     }
   };
 
   if (npages > 0) {
-    load(0, 0);
-    load(1, 1);
+    load(0);
+    put(0, 0);
+    load(1);
   }
   Row row[1];
   row[0].init(a, t, wrow + lr, lg);
@@ -513,19 +601,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EU))) void 
   const int wlast = (min(wrow + 16, wend) - 1) / a.G;
   const bool tree = a.parents != nullptr && a.n > 1;
   if (tree) tree_masks(a, t, masks, par, NT);
-  if (npages > 0) put(0, 0);
   __syncthreads();
 
   auto step = [&](auto masked, int it, int buf) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     const int page = t.beg + it;
-    load(it + 2, buf);
     if (has_rows && !(MASKED && page * kPage > t.L + wlast)) {
       f32x4 sc[1][2] = {{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}};
 #pragma unroll
       for (int s = 0; s < S; ++s)
-        fp4_score_step(row, s, *(const bf16x8*)&tile[buf][(2 * s) * 64 + lane],
-                       *(const bf16x8*)&tile[buf][(2 * s + 1) * 64 + lane], sc);
+        fp4_score_step(row, s, *(const bf16x8*)&tile[buf][(2 * s) * 64 + Pieces::turned(lane, s)],
+                       *(const bf16x8*)&tile[buf][(2 * s + 1) * 64 + Pieces::turned(lane, s)], sc);
       unsigned none = 0;
       if (MASKED && (page + 1) * kPage > t.L) {
         const unsigned g0 = *(const unsigned*)&gone[buf][4 * lg], g1 = *(const unsigned*)&gone[buf][16 + 4 * lg];
@@ -535,10 +621,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EU))) void 
       fp4_softmax<MASKED>(row, sc, page_bad[buf], none, tree, page * kPage - t.L, t.node0, masks, lg, pf);
 #pragma unroll
       for (int d = 0; d < DT; d += 2)
-        value_step(row, d, *(const bf16x8*)&tile[buf][(2 * S + d) * 64 + lane],
-                   *(const bf16x8*)&tile[buf][(2 * S + d + 1) * 64 + lane], pf);
+        value_step(row, d, *(const bf16x8*)&tile[buf][(2 * S + d) * 64 + Pieces::turned(lane, d / 2)],
+                   *(const bf16x8*)&tile[buf][(2 * S + d + 1) * 64 + Pieces::turned(lane, d / 2)], pf);
     }
     put(it + 1, buf ^ 1);
+    load(it + 2);
     __syncthreads();
   };
   // Pairs of pages of prompt tokens only, then the pages that hold nodes (and
@@ -558,12 +645,268 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EU))) void 
   row[0].store(a, t, lg);
 }
 
+// A tile of 32 rows in a wave: lane (row lane % 32, half h = lane / 32).
+template <int HD, typename QT>
+struct Fp4Wide {
+  static constexpr int S = HD / 16, DT = HD / 32;
+  static constexpr int QP = sizeof(QT) == 4 ? 3 : 1, PP = QP;
+  bf16x8 q[S][QP];       // dims 16 s + 8 h .. +7
+  f32x16 acc[DT];        // i < 8: dim 32 d + 16 (i / 4) + 8 h + 2 (i % 4); i + 8: the next one
+  Fp4Softmax sm;
+  int node, head;
+  bool valid;
+};
+
+// fp4_many_kernel with tiles of 32 rows (MFMA 32x32x16).  Half the matrix
+// instructions and LDS reads, each page expanded for twice the rows, and more of
+// the vector work beside a matrix instruction, which keeps its SIMD from it for
+// about eight cycles whatever its size.
+// TILES: row tiles of a workgroup, 4 or 2.  With two, a pair of waves shares a
+// tile's rows and takes every other page each; they merge through LDS.
+// Scores: lane (row, h) holds slots 8 j + 4 h + e, j < 4, e < 4, which in that
+// order are its operand of the two value products of 16 slots.
+template <int HD, typename QT, int TILES>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) == 2 && TILES == 4 ? 3 : 2))) void fp4_wide_kernel(TreeAttnArgs a) {
+  using Row = Fp4Wide<HD, QT>;
+  using Pieces = Fp4Pieces<HD>;
+  constexpr int NT = 256, KS = 4 / TILES;            // pages at a time
+  constexpr int S = Row::S, DT = Row::DT, QP = Row::QP, PP = Row::PP;
+  constexpr int ROWS = 32 * TILES;
+  // operands of 64 lanes: keys [S], values [DT][2]
+  struct Tile {
+    u32x4 k[S * 64], v[DT * 2 * 64];
+  };
+  __shared__ __attribute__((aligned(16))) Tile tiles[2][KS];
+  __shared__ __attribute__((aligned(4))) uint8_t gone[2][KS][kPage];     // 1: the slot's value is NaN
+  __shared__ uint32_t masks[ROWS * kTreeWords];
+  __shared__ int par[kTreeMax];
+  static_assert(KS == 1 || sizeof(tiles) >= TILES * (2 + 16 * DT) * 64 * sizeof(float), "room for the merge");
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, h = lane >> 5;
+  const TreeSpan t = tree_span(a, a.wg_tiles);
+  const int rt = (wave + t.turn) % TILES, ks = wave / TILES;   // turned as in fp4_many_kernel
+  if (t.none) return;   // uniform over the workgroup
+  const int npages = t.end - t.beg;
+  const int wrow = t.row0 + 32 * rt;
+  const int wend = min(t.row0 + 16 * a.wg_tiles, t.nrows);
+  const bool has_rows = wrow < wend;
+
+  const int* table = a.c.table + (long long)t.b * a.c.table_stride + t.beg;
+  Pieces pieces;
+  pieces.init(wave);
+  typename Pieces::Raw in[KS];
+  float page_bad[2] = {0.f, 0.f};    // of this wave's page
+  int id_next[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) id_next[k] = npages > 0 ? table[min(k, npages - 1)] : 0;
+  auto load = [&](int st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const int id = id_next[k];
+      id_next[k] = table[min(KS * (st + 1) + k, npages - 1)];
+      in[k].bad = id < 0 || id >= a.c.pages;
+      pieces.load(in[k], a.c.pool + ((long long)(in[k].bad ? 0 : id) * a.c.Hkv + t.kvh) * Pieces::UNIT);
+    }
+  };
+  auto put = [&](int st, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const int page = t.beg + KS * st + k;
+      const bool nodes = (page + 1) * kPage > t.L;
+      Tile& tile = tiles[buf][k];
+      if (k == ks) page_bad[buf] = bad_page(in[k].bad);
+#pragma unroll
+      for (int c = 0; c < Pieces::PER; ++c) {
+        if (!pieces.any(c)) continue;
+        const int s = Pieces::block(c), l = Pieces::lane(c), g = l / 16, x = l % 16;
+        u32x2 w = in[k].codes[c], e = in[k].scales[c];
+        if (pieces.keys(c)) {   // keys x and x + 16, dims 32 s + 8 g .. +7
+          union {
+            bf16x8 b;
+            u32x4 u;
+          } k0, k1;
+          k0.b = fp4_key(w.x, fp4_scale_of(e.x, 0));
+          k1.b = fp4_key(w.y, fp4_scale_of(e.x, 1));
+          u32x4* at = &tile.k[(2 * s + (g >> 1)) * 64 + Pieces::turned((g & 1) * 32 + x, s)];
+          at[0] = k0.u;
+          at[16] = k1.u;
+        } else {   // dims 32 s + 2 x and + 1, slots 4 g .. +3 and 16 + 4 g .. +3
+          if (nodes) Pieces::hold(c, w, e, gone[buf][k], in[k].bad ? 0 : t.L + t.nb - page * kPage);
+          u32x2* at = (u32x2*)&tile.v[2 * s * 64 + Pieces::turned((g & 1) * 32 + x, s)] + (g >> 1);
+          unsigned even[2], odd[2];
+          fp4_values4(w.x, e.x, even, odd);
+          at[0] = (u32x2){even[0], even[1]};
+          at[32] = (u32x2){odd[0], odd[1]};
+          fp4_values4(w.y, e.y, even, odd);
+          at[128] = (u32x2){even[0], even[1]};
+          at[160] = (u32x2){odd[0], odd[1]};
+        }
+      }
+    }
+  };
+
+  if (npages > 0) {
+    load(0);
+    put(0, 0);
+    load(1);
+  }
+  Row row;
+  {
+    const int r0 = wrow + lr;
+    row.valid = r0 < wend;
+    const int r = r0 < t.nrows ? r0 : t.nrows - 1;
+    row.node = r / a.G;
+    row.head = t.kvh * a.G + r % a.G;
+    const QT* qp = (const QT*)a.q + t.b * a.qsb + row.node * a.qst + (long long)row.head * HD + 8 * h;
+#pragma unroll
+    for (int s = 0; s < S; ++s) fp4_q8<QT, QP>(qp + 16 * s, a.scale_log2, row.q[s]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) row.acc[d][i] = 0.f;
+    row.sm.init(a.scale_log2, t.over);
+  }
+  // the last node of the wave's rows: later pages hold nothing for it
+  const int wlast = (min(wrow + 32, wend) - 1) / a.G;
+  const bool tree = a.parents != nullptr && a.n > 1;
+  if (tree) tree_masks(a, t, masks, par, NT);
+  __syncthreads();
+
+  auto step = [&](auto masked, int st, int buf) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const int page = t.beg + KS * st + ks;
+    if (has_rows && !(MASKED && (page * kPage > t.L + wlast || (KS > 1 && page >= t.end)))) {
+      const Tile& tile = tiles[buf][ks];
+      f32x16 sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const bf16x8 k = *(const bf16x8*)&tile.k[s * 64 + Pieces::turned(lane, s / 2)];
+#pragma unroll
+        for (int pl = 0; pl < QP; ++pl)
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, row.q[s][pl], sc, 0, 0, 0);
+      }
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = sc[i];
+      if constexpr (MASKED) {
+        const int i0 = page * kPage - t.L;
+        const unsigned vis = (tree ? slots_of_tree(i0, masks + (row.node - t.node0) * kTreeWords)
+                                   : slots_of_chain(i0, row.node)) >> (4 * h);
+        const bool nodes = i0 + kPage > 0;
+        const float nan = __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const unsigned g = nodes ? *(const unsigned*)&gone[buf][ks][8 * j + 4 * h] : 0u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            p[4 * j + e] = !(vis >> (8 * j + e) & 1u) ? -INFINITY : g >> (8 * e) & 1u ? nan : p[4 * j + e];
+        }
+        row.sm.l += vis & 0x0f0f0f0fu ? page_bad[buf] : 0.f;
+      } else {
+        row.sm.l += page_bad[buf];
+      }
+      row.sm.raise(halves_max(max_of(p)), [&](float c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) row.acc[d] *= c;
+      });
+      row.sm.exps(p);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        bf16x8 pf[PP];
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = p[8 * k + e];
+        fp4_p_planes(w, pf);
+        bf16x8 vf[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) vf[d] = *(const bf16x8*)&tile.v[(2 * d + k) * 64 + Pieces::turned(lane, d)];
+#pragma unroll
+        for (int pl = 0; pl < PP; ++pl)
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+            row.acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d], pf[pl], row.acc[d], 0, 0, 0);
+      }
+    }
+    put(st + 1, buf ^ 1);
+    load(st + 2);
+    __syncthreads();
+  };
+  const int steps = (npages + KS - 1) / KS;
+  const int plain = min(npages, max(0, t.L / kPage - t.beg)) / KS & ~1;
+  int st = 0;
+  for (; st < plain; st += 2) {
+    step(std::false_type{}, st, 0);
+    step(std::false_type{}, st + 1, 1);
+  }
+  for (; st < steps; st += 2) {
+    step(std::true_type{}, st, 0);
+    if (st + 1 < steps) step(std::true_type{}, st + 1, 1);
+  }
+  row.sm.l += __shfl_xor(row.sm.l, 32, 64);
+  if constexpr (KS > 1) {   // the second wave of a pair hands over (the tiles are no longer read)
+    float* x = (float*)tiles + rt * (2 + 16 * DT) * 64;
+    if (ks > 0 && has_rows) {
+      x[lane] = row.sm.m;
+      x[64 + lane] = row.sm.l;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[(2 + 16 * d + i) * 64 + lane] = row.acc[d][i];
+    }
+    __syncthreads();
+    if (ks > 0) return;
+    if (has_rows) {
+      const float mq = x[lane], lq = x[64 + lane];
+      const float mn = fmaxf(row.sm.m, mq);
+      const float s0 = row.sm.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(row.sm.m - mn);
+      const float s1 = mq == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mq - mn);
+      row.sm.l = row.sm.l * s0 + lq * s1;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) row.acc[d][i] = row.acc[d][i] * s0 + x[(2 + 16 * d + i) * 64 + lane] * s1;
+      row.sm.m = mn;
+    }
+  }
+  if (!has_rows || !row.valid) return;
+  const bool whole = t.parts == 1;
+  const float inv = whole ? 1.f / row.sm.l : 1.f;
+  const long long out = ((long long)t.b * a.n + row.node) * a.H + row.head;
+  const long long prow = ((long long)t.slot * a.n + row.node) * a.H + row.head;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      f32x4 y[2];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[e / 2][e % 2 * 2] = row.acc[d][4 * j + e] * inv;
+        y[e / 2][e % 2 * 2 + 1] = row.acc[d][8 + 4 * j + e] * inv;
+      }
+      const int at = 32 * d + 16 * j + 8 * h;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (whole) store4<QT>((QT*)a.out + out * HD + at + 4 * u, y[u]);
+        else *(f32x4*)(a.part_o + prow * HD + at + 4 * u) = y[u];
+      }
+    }
+  if (!whole && h == 0) {
+    a.part_ml[prow * 2] = row.sm.m;
+    a.part_ml[prow * 2 + 1] = row.sm.l;
+  }
+}
+
 template <int HD, typename QT>
 hipError_t fp4_attn_rows(const TreeAttnArgs& a, const TreeAttnPlan& p, hipStream_t st) {
   const unsigned grid = (unsigned)((long long)p.row_groups * p.slots * a.c.Hkv);
   if (p.few == 1) fp4_few_kernel<HD, QT, 1><<<grid, 256, 0, st>>>(a);
   else if (p.few == 2) fp4_few_kernel<HD, QT, 2><<<grid, 256, 0, st>>>(a);
-  else fp4_many_kernel<HD, QT, 3><<<grid, 256, 0, st>>>(a);
+  else if (p.paired) fp4_wide_kernel<HD, QT, 2><<<grid, 256, 0, st>>>(a);
+  else if (p.wide) fp4_wide_kernel<HD, QT, 4><<<grid, 256, 0, st>>>(a);
+  else fp4_many_kernel<HD, QT><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == a.c.B) return e;
   const long long rows = (long long)a.c.B * a.n * a.H;

@@ -15,8 +15,9 @@ constexpr int kTreeMaxSplits = 64;
 constexpr int kTreeShared = 64;   // prompts that share the key splits by their lengths
 
 struct TreeAttnPlan {
-  int few;                 // 1, 2: tree_few_kernel with so many row tiles
-  bool wide;               // tree_wide_kernel; else tree_many_kernel
+  int few;                 // 1, 2: *_few_kernel with so many row tiles
+  bool wide;               // *_wide_kernel; else *_many_kernel
+  bool paired;             // 4 bits, wide: two waves a tile
   bool four;               // tree_many_kernel at four waves a SIMD; else three
   int wg_tiles;            // row tiles (of 16) per workgroup
   int row_groups, slots, split_pages;
@@ -25,9 +26,7 @@ struct TreeAttnPlan {
 
 // dtype: 0 fp32, 1 bf16.  fp32 over e4m3 (heads of 128) is as fast in tiles of 16
 // rows (188 us) as of 32 (190).
-constexpr bool tree_may_be_wide(int hd, int dtype, int format) {
-  return format != kMxfp4 && !(hd == 128 && dtype == 0 && format == kE4M3);
-}
+constexpr bool tree_may_be_wide(int hd, int dtype, int format) { return !(hd == 128 && dtype == 0 && format == kE4M3); }
 
 // Four workgroups a CU where there are as many; fewer are faster in three (64
 // trees of 65 at 2048 in bf16: 152 -> 146 us; 16 of them: 56 -> 61).  Heads of 64
@@ -55,10 +54,28 @@ inline TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max
   const long long pairs = (long long)B * Hkv;
   const long long one = (tiles + 3) / 4, two = (tiles + 7) / 8, full = pairs * two;
   const long long pages = ((long long)max_len + n + kPage - 1) / kPage;
-  const bool filled = 16 * (8 * two - tiles) <= 8 * two && (full >= 768 || (dtype == 1 && full >= 448 && full <= 512));
-  const bool split = one == 2 * two && full * 3 <= 512 * 2 && pages >= 128 && full * pages >= 8192;
-  p.wide = !p.few && (filled || split) && tree_may_be_wide(hd, dtype, format);
-  const int most_tiles = p.few ? p.few : p.wide ? 8 : 4;
+  bool filled = 16 * (8 * two - tiles) <= 8 * two && (full >= 768 || (dtype == 1 && full >= 448 && full <= 512));
+  bool split = one == 2 * two && full * 3 <= 512 * 2 && pages >= 128 && full * pages >= 8192;
+  // 4 bits.  Tiles of 32 rows:
+  //  - a tile to two waves, unsplit, where that fills the chip with two workgroups a
+  //    CU and the keys are many but not a whole split's worth (us with tiles of 16
+  //    and so, bf16 and fp32 at heads of 128: two chunks of 509 x 4 over 1000: 47, 43
+  //    and 63, 61; over 3001: 85, 76 and 131, 127; over 8192: 240, 198 and 364, 354,
+  //    where whole tiles over split keys take 185 and 353; 16 trees of 64 x 4 at
+  //    1000: 33, 31 and 47, 45; 16 of 51 at 512: 25.0, 25.4 and 35.4, 36.7);
+  //  - where long keys are split (a chunk of 512 over 32768, two prompts: 847, 580 and
+  //    1313, 1230; 32 trees of 17 at 8192: 236, 152 and 336, 296; 8 of 65, whose 17
+  //    tiles leave the last group part empty: 98, 85 and 145, 154; 4 of 64 at 4000: 38,
+  //    39 and 50, 52);
+  //  - in bf16 where they fill the chip (12 chunks of 500 at 1000: 199, 178 and 330,
+  //    343; 64 trees of 64 at 1024: 111, 105 and 191, 190).
+  if (format == kMxfp4) {
+    p.paired = !p.few && pairs * one >= 448 && pairs * one <= 512 && pages >= 32 && pages < 256;
+    filled = dtype == 1 && 16 * (8 * two - tiles) <= 8 * two && full >= 768;
+    split = (dtype == 1 ? tiles >= 5 * two : one == 2 * two) && full * 3 <= 512 * 2 && pages >= 96 && full * pages >= 13000;
+  }
+  p.wide = !p.few && (filled || split || p.paired) && tree_may_be_wide(hd, dtype, format);
+  const int most_tiles = p.few ? p.few : p.wide && !p.paired ? 8 : 4;
   p.row_groups = (tiles + most_tiles - 1) / most_tiles;
   p.wg_tiles = (tiles + p.row_groups - 1) / p.row_groups;
   // Keys are split until there are two workgroups a CU (few rows, tiles of 32) or
@@ -78,11 +95,16 @@ inline TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max
   // 2048: 27 whole, 31.5).  Few rows over a long cache are split in two whatever
   // their number: one prompt of 16384 among 63 short ones takes 37 us instead of
   // 116, 64 of up to 8192 115 instead of 119.
-  p.split_pages = p.few ? 16 : (int)(4 + ((long long)B * n * H * hd >> 17));
+  // (4 bits, whose pages are half as long: 32 for long prompts; one token at 32768: 19.7
+  // and 17.3 us, 8 prompts of 8 nodes x 4 at 4096: 22.7 and 21.7, one at 2048 12.4 and 13.9)
+  p.split_pages = !p.few ? (int)(4 + ((long long)B * n * H * hd >> 17)) : format == kMxfp4 && pages >= 128 ? 32 : 16;
   long long most = std::min<long long>(std::max<long long>(1, pages / p.split_pages), kTreeMaxSplits);
   if (p.few && pages < (pairs >= 256 ? 128 : 48)) most = 1;
   const bool shared = B > 1 && B <= kTreeShared;
-  long long slots = p.few ? 512 / Hkv : p.wide ? 512 / (Hkv * two) : 768 / (Hkv * one);
+  // (4 bits in bf16: three workgroups of tiles of 32 fit a CU; two are enough where
+  // keys are few: two chunks of 300 over 3001: 70 and 74 us)
+  const int fill = format == kMxfp4 && dtype == 1 && pages >= 192 ? 768 : 512;
+  long long slots = p.few ? 512 / Hkv : p.paired ? B : p.wide ? fill / (Hkv * two) : 768 / (Hkv * one);
   if (p.few && shared && pages >= 256) slots = std::max(slots, 2ll * B);
   if (!shared || slots < 2 * B && (pages < 128 || 2 * slots < 3 * B)) slots -= slots % B;
   p.slots = (int)std::max<long long>(B, std::min(slots, B * most));
@@ -94,9 +116,11 @@ inline TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max
 
 // Enough for every type and format.
 inline size_t tree_attn_workspace(int B, int n, int H, int Hkv, int hd, int max_len) {
-  // the types decide on the tiles alone: one pair that may have them of 32, one not
-  return std::max(tree_attn_plan(B, n, H, Hkv, hd, max_len, 1, kInt8).workspace,
-                  tree_attn_plan(B, n, H, Hkv, hd, max_len, 0, kE4M3).workspace);
+  // the types decide on the tiles alone: in 8 bits one pair that may have them of 32, one not
+  return std::max({tree_attn_plan(B, n, H, Hkv, hd, max_len, 1, kInt8).workspace,
+                   tree_attn_plan(B, n, H, Hkv, hd, max_len, 0, kE4M3).workspace,
+                   tree_attn_plan(B, n, H, Hkv, hd, max_len, 0, kMxfp4).workspace,
+                   tree_attn_plan(B, n, H, Hkv, hd, max_len, 1, kMxfp4).workspace});
 }
 
 }  // namespace cdsl
