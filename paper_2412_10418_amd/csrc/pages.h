@@ -10,7 +10,7 @@
 namespace cdsl {
 
 constexpr int kForkRows = 512;      // prompts whose tables one launch forks
-constexpr int kPieceWords = 1024;   // 16-byte words that a workgroup copies at a time, at most
+constexpr int kPieceWords = 512;    // 16-byte words that a workgroup copies at a time, at most
 
 // Pages that a run of count tokens behind len others reaches: [first, end), cut
 // at the table's end; and how many of the tokens fit in the table.
