@@ -20,14 +20,17 @@ namespace {
 
 constexpr unsigned kNoValue = 255;   // the scale of a row that is NaN
 
+// Eight values of a row, which is read once: past the caches, so that the codes stay
+// there (24 prompts of up to 2047 x 8 heads in bf16, written and read back: 55 -> 45 us;
+// 16 of 256 x 32 in fp32: 62 -> 59).
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
   if constexpr (sizeof(T) == 2) {
-    const bf16x8 t = *(const bf16x8*)p;
+    const bf16x8 t = __builtin_nontemporal_load((const bf16x8*)p);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (float)t[e];
   } else {
-    const f32x4 t0 = *(const f32x4*)p, t1 = *(const f32x4*)(p + 4);
+    const f32x4 t0 = __builtin_nontemporal_load((const f32x4*)p), t1 = __builtin_nontemporal_load((const f32x4*)(p + 4));
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = e < 4 ? t0[e & 3] : t1[e & 3];
   }
