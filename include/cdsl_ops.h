@@ -347,7 +347,7 @@ int cdsl_op_pages_compact(const cdsl_kvq* cache, int32_t* table, int32_t* refs,
  * layers, i < n; a pair with an id outside its pool is passed over.  The caches
  * have one format and the same layers and heads (pages, and tables, which are not
  * read, may differ).  A page that is written must be no other pair's dst or, in
- * one pool, src. */
+ * one pool, src.  Pools that overlap otherwise than as one are EINVAL. */
 int cdsl_op_pages_copy(const cdsl_kvq* from, const int32_t* src,
                        const cdsl_kvq* to, const int32_t* dst, int32_t n,
                        void* stream);

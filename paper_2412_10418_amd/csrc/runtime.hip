@@ -1965,9 +1965,18 @@ bool pages_entries_fit(int32_t batch, int32_t max_count) {
   return (long long)batch * (max_count / kPage + 2LL) <= (1 << 30);
 }
 
-int workspace_check(const void* workspace, size_t have, size_t need) {
+struct Ints {
+  const int32_t* p;
+  int64_t n;
+};
+
+// CDSL_OK, or the error of a workspace of which `need` bytes are used, beside a call's arrays
+int workspace_check(const void* workspace, size_t have, size_t need, std::initializer_list<Ints> arrays) {
   if (need > 0 && (!workspace || have < need)) return fail(nullptr, CDSL_EINVAL, "workspace too small");
   if (!aligned16(workspace)) return fail(nullptr, CDSL_EINVAL, "the workspace must be 16-byte aligned");
+  for (const Ints& x : arrays)
+    if (need > 0 && overlap((const int32_t*)workspace, (int64_t)(need / 4), x.p, x.n))
+      return fail(nullptr, CDSL_EINVAL, "the workspace must not overlap an array of the call");
   return CDSL_OK;
 }
 
@@ -2125,7 +2134,8 @@ int cdsl_op_pages_fork(const cdsl_kvq* cache, int32_t* table, int32_t* refs, con
     if (!apart(cache, table, refs, parents, cache->batch))
       return fail(nullptr, CDSL_EINVAL, "parents must not overlap table or refs");
     const size_t need = cache->batch > kForkRows ? 4 * (size_t)cache->batch * cache->table_stride : 0;
-    rc = workspace_check(workspace, workspace_bytes, need);
+    const int64_t B = cache->batch;
+    rc = workspace_check(workspace, workspace_bytes, need, {{table, B * cache->table_stride}, {refs, cache->pages}, {parents, B}});
     if (rc != CDSL_OK) return rc;
     return launched(pages_fork_launch(pages_args(cache, table, refs), parents, (int*)workspace, (hipStream_t)stream));
   });
@@ -2144,7 +2154,8 @@ int cdsl_op_pages_reserve(const cdsl_kvq* cache, int32_t* table, int32_t* refs, 
         overlap(got, B, lens, B) || overlap(got, B, count, B))
       return fail(nullptr, CDSL_EINVAL, "lens, count and got must not overlap table or refs, nor got the others");
     if (!pages_entries_fit(cache->batch, max_count)) return fail(nullptr, CDSL_ERANGE, "too many pages at once");
-    rc = workspace_check(workspace, workspace_bytes, 4 * (size_t)reserve_space(cache->batch, cache->pages, max_count).ints);
+    rc = workspace_check(workspace, workspace_bytes, 4 * (size_t)reserve_space(cache->batch, cache->pages, max_count).ints,
+                         {{table, B * cache->table_stride}, {refs, cache->pages}, {lens, B}, {count, B}, {got, B}});
     if (rc != CDSL_OK) return rc;
     return launched(pages_reserve_launch(pages_args(cache, table, refs), lens, count, max_count, got, (int*)workspace,
                                          (hipStream_t)stream));
@@ -2170,7 +2181,8 @@ int cdsl_op_pages_compact(const cdsl_kvq* cache, int32_t* table, int32_t* refs, 
     if (rc != CDSL_OK) return rc;
     if (!refs || !used) return fail(nullptr, CDSL_EINVAL, "null argument");
     if (!apart(cache, table, refs, used, 1)) return fail(nullptr, CDSL_EINVAL, "used must not overlap table or refs");
-    rc = workspace_check(workspace, workspace_bytes, 4 * (size_t)compact_space(cache->pages).ints);
+    rc = workspace_check(workspace, workspace_bytes, 4 * (size_t)compact_space(cache->pages).ints,
+                         {{table, (int64_t)cache->batch * cache->table_stride}, {refs, cache->pages}, {used, 1}});
     if (rc != CDSL_OK) return rc;
     return launched(pages_compact_launch(pages_args(cache, table, refs), used, (int*)workspace, (hipStream_t)stream));
   });
@@ -2188,6 +2200,10 @@ int cdsl_op_pages_copy(const cdsl_kvq* from, const int32_t* src, const cdsl_kvq*
     if (from->n_layers != to->n_layers || from->n_kv_heads != to->n_kv_heads || from->head_dim != to->head_dim ||
         from->format != to->format)
       return fail(nullptr, CDSL_EINVAL, "the caches' layers, heads or formats differ");
+    const uintptr_t a = (uintptr_t)from->pool, b = (uintptr_t)to->pool;
+    const bool one = a == b && from->pages == to->pages;
+    if (!one && a < b + (uintptr_t)(to->n_layers * kvq_layer_bytes(to)) && b < a + (uintptr_t)(from->n_layers * kvq_layer_bytes(from)))
+      return fail(nullptr, CDSL_EINVAL, "pools that overlap must be one pool of as many pages");
     if (n == 0) return CDSL_OK;
     if (!src || !dst) return fail(nullptr, CDSL_EINVAL, "null argument");
     return launched(pages_copy_launch(pages_args(from, nullptr, nullptr), src, (uint8_t*)to->pool, to->pages,

@@ -87,6 +87,25 @@ def test_null_and_overlapping_arrays():
     assert _copy(c, src=None) == _copy(c, dst=None) == _copy(c, n=-1) == CDSL_EINVAL
 
 
+def test_workspaces_apart_from_the_arrays():
+    from paper_2412_10418_amd.binding import CDSL_EINVAL
+    c, big, n = _cache(), _cache(batch=513, table_stride=9), 1 << 15
+    for at in (TABLE, TABLE + 48, REFS, REFS - 16, A, B_, OUT):
+        assert _reserve(c, ws=at, n=n) == CDSL_EINVAL, hex(at)
+    for at in (TABLE, TABLE + 48, REFS, REFS - 16, OUT):
+        assert _compact(c, ws=at, n=n) == CDSL_EINVAL, hex(at)
+    for at in (TABLE, TABLE + 48, REFS, REFS - 16, A):
+        assert _fork(big, ws=at, n=n) == CDSL_EINVAL, hex(at)
+
+
+def test_pools_that_overlap():
+    """Layers of pools that begin together but hold other numbers of pages, or a pool that begins inside another."""
+    from paper_2412_10418_amd.binding import CDSL_EINVAL, CDSL_OK
+    c = _cache()
+    assert _copy(c, _cache(pages=9)) == _copy(c, _cache(pool=P + 16)) == _copy(_cache(pool=P + 16), c) == CDSL_EINVAL
+    assert _copy(c, c, n=0) == _copy(c, _cache(pool=P + (1 << 30)), n=0) == CDSL_OK
+
+
 def test_workspaces():
     from paper_2412_10418_amd.binding import CDSL_EINVAL
     L, c = _lib(), _cache()
