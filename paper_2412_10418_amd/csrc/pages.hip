@@ -28,20 +28,26 @@ __device__ __forceinline__ int parent_entry(const PagesArgs& a, int parent, int 
   return parent >= 0 && parent < a.B ? a.table[(long long)parent * a.P + i] : -1;
 }
 
-// Workgroup = 16 columns of the table, which it holds in LDS, all rows of them,
-// before it writes any: one launch, where a copy of the table takes two.
-__global__ __launch_bounds__(256) void fork_kernel(PagesArgs a, const int* parents) {
-  __shared__ int old[kForkRows * 16];
-  const int col = threadIdx.x & 15, i = blockIdx.x * 16 + col;
+constexpr int kForkThreads = 1024, kForkCols = 4;
+
+// Workgroup = four columns of the table, which it holds in LDS, all rows of them,
+// before it writes any: one launch, where a copy of the table takes two.  A thread an
+// entry, as far as they go: loads and atomics that wait for each other bound it (with 16
+// columns and 256 threads: 64 prompts of 17 pages 5.8 -> 3.3 us, 256 of 65 24 -> 7,
+// 512 of 257 49 -> 16, 512 of 1025 58 -> 48, where the atomics do).
+__global__ __launch_bounds__(kForkThreads) void fork_kernel(PagesArgs a, const int* parents) {
+  constexpr int COLS = kForkCols;
+  __shared__ int old[kForkRows * COLS];
+  const int col = threadIdx.x % COLS, i = blockIdx.x * COLS + col, rows = blockDim.x / COLS;
   if (i < a.P)
-    for (int b = threadIdx.x >> 4; b < a.B; b += 16) old[b * 16 + col] = a.table[(long long)b * a.P + i];
+    for (int b = threadIdx.x / COLS; b < a.B; b += rows) old[b * COLS + col] = a.table[(long long)b * a.P + i];
   __syncthreads();
   if (i >= a.P) return;
-  for (int b = threadIdx.x >> 4; b < a.B; b += 16) {
+  for (int b = threadIdx.x / COLS; b < a.B; b += rows) {
     const int p = parents[b];
     if (p == b) continue;
-    const int now = p >= 0 && p < a.B ? old[p * 16 + col] : -1;
-    hold(a.refs, a.pages, old[b * 16 + col], now);
+    const int now = p >= 0 && p < a.B ? old[p * COLS + col] : -1;
+    hold(a.refs, a.pages, old[b * COLS + col], now);
     a.table[(long long)b * a.P + i] = now;
   }
 }
@@ -508,7 +514,8 @@ CopyArgs copy_within(const PagesArgs& a, const int* src, const int* dst, const i
 hipError_t pages_fork_launch(const PagesArgs& a, const int* parents, int* workspace, hipStream_t st) {
   if (a.B == 0) return hipSuccess;
   if (a.B <= kForkRows) {
-    fork_kernel<<<(unsigned)((a.P + 15) / 16), 256, 0, st>>>(a, parents);
+    const int threads = std::min((a.B * kForkCols + 63) / 64 * 64, kForkThreads);
+    fork_kernel<<<(unsigned)((a.P + kForkCols - 1) / kForkCols), threads, 0, st>>>(a, parents);
     return hipGetLastError();
   }
   const dim3 grid((unsigned)std::min((a.P + 255) / 256, 64), (unsigned)a.B);
