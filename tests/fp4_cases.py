@@ -39,3 +39,14 @@ ALL = [
 def params():
     import pytest
     return [pytest.param(c, k, id=f"{c.name}-{k}".replace(" ", "_")) for c in ALL for k in KINDS]
+
+
+# Unsplit prompts of so many pages that a wave takes page ids more than once (64 at a time): first and last are long, the rest
+# hold a token.  (B, n, H, KV heads, head dim, longest)
+MANY_PAGES = [
+    Case("few1 long", 70, 1, 8, 8, 32, 9000, None, "few1"),
+    Case("few2 long", 70, 20, 8, 8, 64, 9000, None, "few2"),
+    Case("many long", 70, 40, 8, 8, 64, 4200, None, "many"),
+    Case("paired long", 28, 32, 32, 8, 64, 4400, None, "paired"),
+    Case("wide long", 96, 32, 32, 8, 32, 4200, None, _bf16("wide", "many")),
+]

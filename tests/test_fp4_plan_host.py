@@ -7,7 +7,7 @@ import subprocess
 
 import pytest
 
-from fp4_cases import ALL
+from fp4_cases import ALL, MANY_PAGES
 from tree_cases import KINDS
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -21,7 +21,7 @@ def test_shapes_take_the_kernels_that_they_test(tmp_path):
            os.path.join(ROOT, "tests", "native", "fp4_plan_test.cpp"), "-o", str(exe)]
     r = subprocess.run(cmd, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
-    asked = [(c, k) for c in ALL for k in KINDS]
+    asked = [(c, k) for c in ALL + MANY_PAGES for k in KINDS]
     lines = "".join(f"{c.B} {c.n} {c.H} {c.heads} {c.hd} {c.longest} {KINDS.index(k)}\n" for c, k in asked)
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:verify_asan_link_order=0", UBSAN_OPTIONS="print_stacktrace=1")
     r = subprocess.run([str(exe)], input=lines, capture_output=True, text=True, env=env, timeout=120)
