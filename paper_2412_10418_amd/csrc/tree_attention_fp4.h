@@ -107,6 +107,17 @@ __device__ __forceinline__ float max_of(const float (&x)[N]) {
   return m;
 }
 
+// The same over the two lanes of a row that are 32 apart, and over four.
+__device__ __forceinline__ float max_halves(float v) {
+  const u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float(t.x), __uint_as_float(t.y));
+}
+__device__ __forceinline__ float max_groups(float v) {
+  v = max_halves(v);
+  const u32x2 t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float(t.x), __uint_as_float(t.y));
+}
+
 __device__ __forceinline__ unsigned held_mask(int held) {
   return held >= 32 ? ~0u : held <= 0 ? 0u : (1u << held) - 1u;
 }
@@ -227,7 +238,7 @@ struct Fp4Tile {
   // Probabilities of a page as planes, from its scores (slots 4 lg + e and 16 + 4
   // lg + e).
   __device__ __forceinline__ void softmax(float (&s)[8], bf16x8 (&pf)[PP]) {
-    sm.raise(groups_max(max_of(s)), [&](float c) __attribute__((always_inline)) {
+    sm.raise(max_groups(max_of(s)), [&](float c) __attribute__((always_inline)) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[d] *= c;
     });
@@ -307,13 +318,27 @@ __device__ __forceinline__ void fp4_softmax(Row (&row)[RPW], const f32x4 (&sc)[R
     row[r].softmax(s, pf[r]);
   }
 }
-__device__ __forceinline__ float bad_page(bool bad) { return bad ? __uint_as_float(0x7fc00000u) : 0.f; }
 
 // This lane's slots whose value scales are 255, bit e (from the words of block 0).
 __device__ __forceinline__ unsigned fp4_none_bits(unsigned s0, unsigned s1) {
   const unsigned a = fp4_none(s0) >> 7, b = fp4_none(s1) >> 7;
   return (a | a >> 7 | a >> 14 | a >> 21) & 15u | ((b | b >> 7 | b >> 14 | b >> 21) & 15u) << 4;
 }
+
+// The pages of a KV head.
+template <int HD>
+struct Fp4Pages {
+  const uint8_t* base;
+  unsigned pages;
+  unsigned long long stride;
+  __device__ __forceinline__ Fp4Pages(const TreeAttnArgs& a, int kvh)
+      : base(a.c.pool + (long long)kvh * fp4_unit_bytes(HD)), pages(a.c.pages),
+        stride((unsigned long long)a.c.Hkv * fp4_unit_bytes(HD)) {}
+  // What a page's rows add to the sums that see it: 0, or the bits of a NaN if there is
+  // none (its loads take page 0).
+  __device__ __forceinline__ unsigned bad(int id) const { return (unsigned)id < pages ? 0u : 0x7fc00000u; }
+  __device__ __forceinline__ const uint8_t* unit(int id) const { return base + ((unsigned)id < pages ? (unsigned)id : 0u) * stride; }
+};
 
 // Few rows (one or two tiles).  Workgroup = (key split, prompt x KV head, group of
 // RPW row tiles); its four waves take every fourth page each, straight from memory
@@ -331,7 +356,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void f
   constexpr int KW = 4;
   using Row = Fp4Tile<HD, QT, sizeof(QT) == 4 ? 3 : RPW == 1 ? 2 : 1>;
   constexpr int S = Row::S, DT = Row::DT, W = fp4_pair(HD), C = S / W;
-  constexpr int UNIT = fp4_unit_bytes(HD);
   constexpr int SLOT = (2 + 4 * DT) * 64;    // floats a wave hands over per row tile
   constexpr int XF = (KW - 1) * RPW * SLOT, MF = 16 * RPW * kTreeWords + kTreeMax;
   typedef unsigned Chunk __attribute__((ext_vector_type(2 * W)));   // [block][half of the page]
@@ -361,15 +385,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void f
   uint32_t* masks = (uint32_t*)lds;
   if (tree) tree_masks(a, t, masks, (int*)lds + 16 * RPW * kTreeWords, 256);
 
+  const Fp4Pages<HD> pages(a, t.kvh);
   struct Page {
     Chunk k[C], v[C], vs[C];
     Scales ks[C];
-    bool bad;
+    unsigned bad;
   } in;
   auto load = [&](int it) __attribute__((always_inline)) {
     const int id = __builtin_amdgcn_readlane(ids, it & 63);
-    in.bad = id < 0 || id >= a.c.pages;
-    const uint8_t* unit = a.c.pool + ((long long)(in.bad ? 0 : id) * a.c.Hkv + t.kvh) * UNIT;
+    in.bad = pages.bad(id);
+    const uint8_t* unit = pages.unit(id);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       in.k[c] = *((const Chunk*)(unit + c * 1024) + lane);
@@ -411,7 +436,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void f
         }
     }
     bf16x8 pf[RPW][Row::PP];
-    fp4_softmax<MASKED>(row, sc, bad_page(now.bad), none, tree, page * kPage - t.L, t.node0, masks, lg, pf);
+    fp4_softmax<MASKED>(row, sc, __uint_as_float(now.bad), none, tree, page * kPage - t.L, t.node0, masks, lg, pf);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int c = s / W, i = s % W * 2;
@@ -475,10 +500,9 @@ struct Fp4Pieces {
   static constexpr int NT = 256, P = fp4_pair(HD);
   static constexpr int N = 4 * HD;
   static constexpr int PER = (N + NT - 1) / NT;
-  static constexpr int UNIT = fp4_unit_bytes(HD);
   struct Raw {
     u32x2 codes[PER], scales[PER];   // of keys: two bytes of scales in .x
-    bool bad;
+    unsigned bad;
   };
   unsigned at[PER], scale_at[PER];   // offsets in a unit
   int wave;
@@ -562,23 +586,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
   const int* table = a.c.table + (long long)t.b * a.c.table_stride + t.beg;
   // The next page's codes are in flight while one is computed.  (Loads past the last
   // page repeat it.)
+  const Fp4Pages<HD> pages(a, t.kvh);
   Pieces pieces;
   pieces.init(wave);
   typename Pieces::Raw in;
   // Page ids are read 64 at a time, one a lane: read one by one, a step ahead, each is waited
-  // for behind the barrier (64 trees of 65 at heads of 64 in fp32: 146 -> 138 us; at 128 234 ->
-  // 231, 32 trees of 17 at 8192 in bf16 104 -> 102).
+  // for behind the barrier (64 trees of 65 in bf16 142 -> 140 us, in fp32 234 -> 231).
   int ids = 0;
   auto load = [&](int it) __attribute__((always_inline)) {
     if ((it & 63) == 0) ids = table[min(it + lane, npages - 1)];
     const int id = __builtin_amdgcn_readlane(ids, it & 63);
-    in.bad = id < 0 || id >= a.c.pages;
-    pieces.load(in, a.c.pool + ((long long)(in.bad ? 0 : id) * a.c.Hkv + t.kvh) * Pieces::UNIT);
+    in.bad = pages.bad(id);
+    pieces.load(in, pages.unit(id));
   };
   float page_bad[2] = {0.f, 0.f};
   auto put = [&](int it, int buf) __attribute__((always_inline)) {
     const int page = t.beg + it;
-    page_bad[buf] = bad_page(in.bad);
+    page_bad[buf] = __uint_as_float(in.bad);
     const bool nodes = (page + 1) * kPage > t.L;
 #pragma unroll
     for (int c = 0; c < Pieces::PER; ++c) {
@@ -729,6 +753,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
   const bool has_rows = wrow < wend;
 
   const int* table = a.c.table + (long long)t.b * a.c.table_stride + t.beg;
+  const Fp4Pages<HD> pages(a, t.kvh);
   Pieces pieces;
   pieces.init(wave);
   typename Pieces::Raw in[KS];
@@ -739,8 +764,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       const int id = __builtin_amdgcn_readlane(ids, (KS * st + k) & 63);
-      in[k].bad = id < 0 || id >= a.c.pages;
-      pieces.load(in[k], a.c.pool + ((long long)(in[k].bad ? 0 : id) * a.c.Hkv + t.kvh) * Pieces::UNIT);
+      in[k].bad = pages.bad(id);
+      pieces.load(in[k], pages.unit(id));
     }
   };
   auto put = [&](int st, int buf) __attribute__((always_inline)) {
@@ -749,7 +774,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
       const int page = t.beg + KS * st + k;
       const bool nodes = (page + 1) * kPage > t.L;
       Tile& tile = tiles[buf][k];
-      if (k == ks) page_bad[buf] = bad_page(in[k].bad);
+      if (k == ks) page_bad[buf] = __uint_as_float(in[k].bad);
 #pragma unroll
       for (int c = 0; c < Pieces::PER; ++c) {
         if (!pieces.any(c)) continue;
@@ -857,7 +882,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
       } else {
         row.sm.l += page_bad[buf];
       }
-      row.sm.raise(halves_max(max_of(p)), [&](float c) __attribute__((always_inline)) {
+      row.sm.raise(max_halves(max_of(p)), [&](float c) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) row.acc[d] *= c;
       });
