@@ -292,12 +292,13 @@ __device__ __forceinline__ void fp4_score_step(const Row (&row)[RPW], int s, con
 }
 
 // Planes of p of every row tile of a wave, from a page's scores.  MASKED: the
-// page holds nodes.  none: this lane's slots whose values are NaN (bit e).  bad: NaN
+// page holds nodes; all: the rows see all of it, and no value is NaN.  none: this
+// lane's slots whose values are NaN (bit e).  bad: NaN
 // for a page that does not exist, which the sums of the rows that see a slot of it
 // take up; else 0.
 template <bool MASKED, typename Row, int RPW>
 __device__ __forceinline__ void fp4_softmax(Row (&row)[RPW], const f32x4 (&sc)[RPW][2], float bad, unsigned none,
-                                            bool tree, int i0, int node0, const uint32_t* masks, int lg,
+                                            bool all, bool tree, int i0, int node0, const uint32_t* masks, int lg,
                                             bf16x8 (&pf)[RPW][Row::PP]) {
   const float nan = __uint_as_float(0x7fc00000u);
 #pragma unroll
@@ -305,7 +306,7 @@ __device__ __forceinline__ void fp4_softmax(Row (&row)[RPW], const f32x4 (&sc)[R
     float s[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] = sc[r][e >> 2][e & 3];
-    if constexpr (MASKED) {
+    if (MASKED && !all) {
       const unsigned vis = (tree ? slots_of_tree(i0, masks + (row[r].node - node0) * kTreeWords)
                                  : slots_of_chain(i0, row[r].node)) >> (4 * lg);
 #pragma unroll
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void f
         }
     }
     bf16x8 pf[RPW][Row::PP];
-    fp4_softmax<MASKED>(row, sc, __uint_as_float(now.bad), none, tree, page * kPage - t.L, t.node0, masks, lg, pf);
+    fp4_softmax<MASKED>(row, sc, __uint_as_float(now.bad), none, false, tree, page * kPage - t.L, t.node0, masks, lg, pf);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int c = s / W, i = s % W * 2;
@@ -576,7 +577,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lg = lane >> 4;
-  const TreeSpan t = tree_span(a, a.wg_tiles);
+  const TreeSpan t = tree_span<true>(a, a.wg_tiles);
   if (t.none) return;   // uniform over the workgroup
   const int npages = t.end - t.beg;
   const int wrow = t.row0 + 16 * ((wave + t.turn) % W);   // where tiles are missing, not always the same SIMD's
@@ -635,8 +636,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
   Row row[1];
   row[0].init(a, t, wrow + lr, lg);
   row[0].valid = wrow + lr < wend;
-  // the last node of the wave's rows: later pages hold nothing for it
-  const int wlast = (min(wrow + 16, wend) - 1) / a.G;
+  // The first and the last node of the wave's rows: in a chunk, pages up to the one are
+  // seen by all of them and take no mask (12 chunks of 500 x 4 rows over 1000 in fp32
+  // 348 -> 340 us), pages past the other by none.
+  const int wfirst = wrow / a.G, wlast = (min(wrow + 16, wend) - 1) / a.G;
   const bool tree = a.parents != nullptr && a.n > 1;
   if (tree) tree_masks(a, t, masks, par, NT);
   __syncthreads();
@@ -671,7 +674,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
         none = (g0 | g0 >> 7 | g0 >> 14 | g0 >> 21) & 15u | ((g1 | g1 >> 7 | g1 >> 14 | g1 >> 21) & 15u) << 4;
       }
       bf16x8 pf[1][Row::PP];
-      fp4_softmax<MASKED>(row, sc, page_bad[buf], none, tree, page * kPage - t.L, t.node0, masks, lg, pf);
+      const int i0 = page * kPage - t.L;
+      const bool all = MASKED && !tree && i0 + kPage - 1 <= wfirst && !__any(none != 0);
+      fp4_softmax<MASKED>(row, sc, page_bad[buf], none, all, tree, i0, t.node0, masks, lg, pf);
 #pragma unroll
       for (int s = 0; s < S; ++s) {
         __builtin_amdgcn_sched_barrier(0);
@@ -720,9 +725,9 @@ struct Fp4Wide {
 // 72 bytes a lane.)
 // TILES: row tiles of a workgroup, 4 or 2.  With two, a pair of waves shares a
 // tile's rows and takes every other page each; they merge through LDS.  (Two chunks of
-// 509 over 3001, lengths alike, in bf16: 94 us; whole tiles, one wave a SIMD, 102, over
-// two splits of the keys with their merge 105.  Waves with two tiles of rows, which
-// halve the reads of LDS again, take 126.)
+// 509 over 3001, lengths alike, in bf16: 90 us.  Before a CU had groups of either end,
+// 94; whole tiles, one wave a SIMD, then took 102, over two splits of the keys with their
+// merge 105, and waves with two tiles of rows, which halve the reads of LDS again, 126.)
 // Scores: lane (row, h) holds slots 8 j + 4 h + e, j < 4, e < 4, which in that
 // order are its operand of the two value products of 16 slots.
 template <int HD, typename QT, int TILES>
@@ -744,7 +749,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, h = lane >> 5;
-  const TreeSpan t = tree_span(a, a.wg_tiles);
+  const TreeSpan t = tree_span<true>(a, a.wg_tiles);
   const int rt = (wave + t.turn) % TILES, ks = wave / TILES;   // turned as in fp4_many_kernel
   if (t.none) return;   // uniform over the workgroup
   const int npages = t.end - t.beg;
@@ -826,12 +831,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
       for (int i = 0; i < 16; ++i) row.acc[d][i] = 0.f;
     row.sm.init(a.scale_log2, t.over);
   }
-  // the last node of the wave's rows: later pages hold nothing for it
-  const int wlast = (min(wrow + 32, wend) - 1) / a.G;
+  // as in fp4_many_kernel (12 chunks of 500 x 4 rows over 1000 in bf16: 183 -> 172 us, one of
+  // 1000 alone 33.5 -> 29.6)
+  const int wfirst = wrow / a.G, wlast = (min(wrow + 32, wend) - 1) / a.G;
   const bool tree = a.parents != nullptr && a.n > 1;
   if (tree) tree_masks(a, t, masks, par, NT);
   __syncthreads();
 
+  // whether a value of this wave's page, of the chunk itself, is NaN
+  auto gone_any = [&](int st, int buf) __attribute__((always_inline)) {
+    return (t.beg + KS * st + ks + 1) * kPage > t.L && __any(gone[buf][ks][lr]);
+  };
   auto step = [&](auto masked, int st, int buf) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     const int page = t.beg + KS * st + ks;
@@ -865,8 +875,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
       float p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = sc[i];
-      if constexpr (MASKED) {
-        const int i0 = page * kPage - t.L;
+      const int i0 = page * kPage - t.L;
+      if (MASKED && (tree || i0 + kPage - 1 > wfirst || gone_any(st, buf))) {
         const unsigned vis = (tree ? slots_of_tree(i0, masks + (row.node - t.node0) * kTreeWords)
                                    : slots_of_chain(i0, row.node)) >> (4 * h);
         const bool nodes = i0 + kPage > 0;
