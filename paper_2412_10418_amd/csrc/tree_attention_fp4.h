@@ -558,9 +558,9 @@ struct Fp4Pieces {
 // tiles); wave w takes tile w.  A page is expanded once for all waves: its codes
 // come in two pages before they are needed and go to LDS as bf16 in operand order.
 //
-// Issue bounds it: 64 trees of 65 x 4 rows over 2048 tokens in fp32 (203 to 235 us) have
+// Issue bounds it: 64 trees of 65 x 4 rows over 2048 tokens in fp32 (200 to 235 us) have
 // vector instructions at 56% of the SIMDs' cycles and matrix ones, six products for the
-// formula's two, at 49%; the two add up.  Workgroups of six or eight waves and four
+// formula's two, at 51%; the two add up.  Workgroups of six or eight waves and four
 // workgroups a CU in fp32 gain nothing.
 template <int HD, typename QT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) == 4 ? 3 : 4))) void fp4_many_kernel(TreeAttnArgs a) {
