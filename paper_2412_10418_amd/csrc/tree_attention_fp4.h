@@ -178,10 +178,10 @@ __device__ __forceinline__ void fp4_q8(const QT* p, float scale, bf16x8 (&q)[QP]
 // A row's running maximum and sum.  The maximum may lag by kLazy, so that O is
 // rescaled rarely; O / l does not depend on it.
 struct Fp4Softmax {
-  float rm;            // log2 units of a score; it meets the -inf of hidden slots, so it is above 0
+  float rm;            // log2 units of a score; it meets the -inf of hidden slots, so a scale of 0 (whose scores are 0) counts 1
   float m, l;          // running maximum (log2 units; -inf before the first visible key), this lane's part of the sum
   __device__ __forceinline__ void init(float scale, bool over) {
-    rm = fmaxf(fabsf(scale), 0x1p-126f);
+    rm = scale == 0.f ? 1.f : fabsf(scale);
     m = -INFINITY;
     l = over ? __uint_as_float(0x7fc00000u) : 0.f;
   }
