@@ -2068,7 +2068,8 @@ int cdsl_op_tree_attention(const cdsl_kvq* cache, int32_t layer, const void* Q, 
     a.n = n;
     a.H = H;
     a.G = H / cache->n_kv_heads;
-    a.scale_log2 = std::min(std::max(scale * 1.4426950408889634f, -FLT_MAX), FLT_MAX);
+    // apart, so that the product neither overflows nor loses bits below the normal numbers
+    a.scale_log2 = std::frexp(scale, &a.scale_exp) * 1.4426950408889634f;
     return launched(tree_attn_launch(a, p, dtype, workspace, (hipStream_t)stream));
   });
 }

@@ -38,7 +38,8 @@ struct TreeAttnArgs {
   const int* n_nodes;      // null: n
   const int* parents;      // null: causal
   int n, H, G;
-  float scale_log2;        // softmax scale * log2(e)
+  float scale_log2;        // softmax scale * log2(e) = scale_log2 * 2^scale_exp, 0.72 <= |scale_log2| < 1.45 or 0
+  int scale_exp;
   float* part_o;           // [slots][n * H][hd]
   float* part_ml;          // [slots][n * H][2]
   int slots, row_groups;   // key splits of all prompts (B: no splits)

@@ -319,12 +319,12 @@ __device__ __forceinline__ void load_q8(const QT* p, float (&x)[8]) {
 struct QScale {
   float down, rm;
 };
-__device__ __forceinline__ QScale q_scale(float scale_log2, unsigned top) {
+__device__ __forceinline__ QScale q_scale(float scale_log2, int scale_exp, unsigned top) {
   const float s = fabsf(scale_log2);
   // s >= 2^(x - 1), x the exponent of frexp
-  const int e = max(max((int)(top >> 23) - 127, -112), -125 - __builtin_amdgcn_frexp_expf(s));
+  const int e = max(max((int)(top >> 23) - 127, -112), -125 - (__builtin_amdgcn_frexp_expf(s) + scale_exp));
   return {__builtin_ldexpf(scale_log2 < 0.f ? -1.f : scale_log2 > 0.f ? 1.f : 0.f, 14 - e),
-          s == 0.f ? 1.f : fminf(__builtin_ldexpf(s, e), 3.4028234663852886e38f)};
+          s == 0.f ? 1.f : fminf(__builtin_ldexpf(s, e + scale_exp), 3.4028234663852886e38f)};
 }
 template <int QP>
 __device__ __forceinline__ void q_planes(const float (&x)[8], float down, f16x8 (&q)[QP]) {
@@ -403,7 +403,7 @@ struct RowTile {
     }
     top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
     top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
-    const QScale qs = q_scale(a.scale_log2, top);
+    const QScale qs = q_scale(a.scale_log2, a.scale_exp, top);
     rm = qs.rm;
 #pragma unroll
     for (int s = 0; s < S; ++s) q_planes<QP>(x[s], qs.down, q[s]);
@@ -949,7 +949,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
       for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[s][e]) & 0x7fffffffu);
     }
     top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
-    const QScale qs = q_scale(a.scale_log2, top);
+    const QScale qs = q_scale(a.scale_log2, a.scale_exp, top);
     row.rm = qs.rm;
 #pragma unroll
     for (int s = 0; s < S; ++s) q_planes<QP>(x[s], qs.down, row.q[s]);

@@ -181,7 +181,7 @@ struct Fp4Softmax {
   float rm;            // log2 units of a score; it meets the -inf of hidden slots, so a scale of 0 (whose scores are 0) counts 1
   float m, l;          // running maximum (log2 units; -inf before the first visible key), this lane's part of the sum
   __device__ __forceinline__ void init(float scale, bool over) {
-    rm = scale == 0.f ? 1.f : fabsf(scale);
+    rm = scale == 0.f ? 1.f : fminf(fabsf(scale), 3.4028234663852886e38f);
     m = -INFINITY;
     l = over ? __uint_as_float(0x7fc00000u) : 0.f;
   }
@@ -233,7 +233,7 @@ struct Fp4Tile {
     for (int s = 0; s < S; ++s) fp4_q8<QT, QP>(qp + 32 * s, a.scale_log2, q[s]);
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    sm.init(a.scale_log2, t.over);
+    sm.init(__builtin_ldexpf(a.scale_log2, a.scale_exp), t.over);
   }
   // Probabilities of a page as planes, from its scores (slots 4 lg + e and 16 + 4
   // lg + e).
@@ -829,7 +829,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) row.acc[d][i] = 0.f;
-    row.sm.init(a.scale_log2, t.over);
+    row.sm.init(__builtin_ldexpf(a.scale_log2, a.scale_exp), t.over);
   }
   // as in fp4_many_kernel (12 chunks of 500 x 4 rows over 1000 in bf16: 183 -> 172 us, one of
   // 1000 alone 33.5 -> 29.6)
