@@ -213,8 +213,8 @@ int cdsl_op_kvq_read(const cdsl_kvq* cache, int32_t layer, void* K, void* V,
  * probabilities of a bf16 call, which are rounded to bf16 (to twice its bits
  * where n * H / n_kv_heads is 16 or less), and for entries of Q below 2^-15
  * (bf16: 2^-31) of their row's largest, which are off by up to 2^-39 of that.
- * Over CDSL_KVQ_MXFP4 no entry of Q is off: it enters as it is, times keys as
- * they are, and scale multiplies the sum.
+ * Over CDSL_KVQ_MXFP4 only entries of Q below 2^-103 of their row's largest are
+ * off, by up to 2^-126 of that.
  * They overflow as in fp32, before the division by the sum of the probabilities
  * (the largest of which counts 1 to 2^8) and with rows of Q scaled to entries
  * below 2: keys, and values times the number of keys, stay below 2^119.

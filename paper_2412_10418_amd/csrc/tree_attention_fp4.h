@@ -14,11 +14,12 @@
 // trade halves: lane x has dims 32 s + 2 x and + 1 of block s, in the tiles "even"
 // and "odd", and a lane's sums of both are eight neighbouring dims of the result.
 //
-// Precision.  q is taken as bf16 planes, exact: three for fp32, one for bf16; the
-// softmax scale multiplies the score.  Probabilities (1 to 2^8 at most, see kLazy)
-// are planes as over 8 bits: three for fp32; for bf16 two with one tile of rows,
-// and one (2^-8 of each, 0.0023 of the result in the mean square where its own
-// rounding is 0.0017) with more.
+// Precision.  A row of q is scaled by a power of two to a largest entry in [1, 2), so
+// that its scores stay within fp32 wherever those of ordinary size do, and taken as bf16
+// planes, three for fp32, one for bf16: exact down to 2^-103 of the largest entry.
+// Probabilities (1 to 2^8 at most, see kLazy) are planes as over 8 bits: three for fp32;
+// for bf16 two with one tile of rows, and one (2^-8 of each, 0.0023 of the result in the
+// mean square where its own rounding is 0.0017) with more.
 #pragma once
 #include "tree_attention.h"
 
@@ -158,15 +159,24 @@ __device__ __forceinline__ void fp4_p_planes(float (&w)[8], bf16x8 (&pf)[PP]) {
   p_planes<PP>(w, pf);
 }
 
-// q as bf16 planes, with the sign of the softmax scale (zeros for a scale of 0): of
-// fp32 three of eight bits, by truncation, of bf16 itself.
-template <typename QT, int QP>
-__device__ __forceinline__ void fp4_q8(const QT* p, float scale, bf16x8 (&q)[QP]) {
-  float x[8];
-  load_q8<QT>(p, x);
-  const float by = scale < 0.f ? -1.f : scale > 0.f ? 1.f : 0.f;
+// The power of two 2^-e that brings a row of q to a largest entry in [1, 2), from the
+// largest bit pattern of |q|: what the entries are multiplied by (with the sign of the
+// softmax scale; 0 for a scale of 0), and what a score of the result counts in log2
+// units, |scale| 2^e.  The former is finite from e = -126 on.  The latter meets the -inf
+// of hidden slots and scores of 0, so e keeps it within 2^-126 and 2^127.  (Where the
+// first of these raises e, entries lose more, and scores 2^-125 at most.)  A NaN or an infinity stays one.
+__device__ __forceinline__ QScale fp4_q_scale(float scale_log2, int scale_exp, unsigned top) {
+  const float s = fabsf(scale_log2);
+  const int x = __builtin_amdgcn_frexp_expf(s) + scale_exp;   // 2^(x - 1) <= |scale| < 2^x
+  const int e = min(max(max((int)(top >> 23) - 127, -126), -125 - x), 127 - x);
+  return {__builtin_ldexpf(scale_log2 < 0.f ? -1.f : scale_log2 > 0.f ? 1.f : 0.f, -e),
+          s == 0.f ? 1.f : __builtin_ldexpf(s, e + scale_exp)};
+}
+// Eight entries as bf16 planes: of fp32 three of eight bits, by truncation, of bf16 itself.
+template <int QP>
+__device__ __forceinline__ void fp4_q8(float (&x)[8], float down, bf16x8 (&q)[QP]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] *= by;
+  for (int e = 0; e < 8; ++e) x[e] *= down;
   if constexpr (QP == 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) q[0][e] = (bf16)x[e];
@@ -175,13 +185,24 @@ __device__ __forceinline__ void fp4_q8(const QT* p, float scale, bf16x8 (&q)[QP]
   }
 }
 
+// The largest bit pattern of |x| among a lane's entries.
+template <int S>
+__device__ __forceinline__ unsigned top_of(const float (&x)[S][8]) {
+  unsigned top = 0;
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[s][e]) & 0x7fffffffu);
+  return top;
+}
+
 // A row's running maximum and sum.  The maximum may lag by kLazy, so that O is
 // rescaled rarely; O / l does not depend on it.
 struct Fp4Softmax {
-  float rm;            // log2 units of a score; it meets the -inf of hidden slots, so a scale of 0 (whose scores are 0) counts 1
+  float rm;            // log2 units of a score, above 0
   float m, l;          // running maximum (log2 units; -inf before the first visible key), this lane's part of the sum
-  __device__ __forceinline__ void init(float scale, bool over) {
-    rm = scale == 0.f ? 1.f : fminf(fabsf(scale), 3.4028234663852886e38f);
+  __device__ __forceinline__ void init(float units, bool over) {
+    rm = units;
     m = -INFINITY;
     l = over ? __uint_as_float(0x7fc00000u) : 0.f;
   }
@@ -229,11 +250,18 @@ struct Fp4Tile {
     node = r / a.G;
     head = t.kvh * a.G + r % a.G;
     const QT* qp = (const QT*)a.q + t.b * a.qsb + node * a.qst + (long long)head * HD + 8 * lg;
+    float x[S][8];
 #pragma unroll
-    for (int s = 0; s < S; ++s) fp4_q8<QT, QP>(qp + 32 * s, a.scale_log2, q[s]);
+    for (int s = 0; s < S; ++s) load_q8<QT>(qp + 32 * s, x[s]);
+    unsigned top = top_of(x);
+    top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
+    top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
+    const QScale qs = fp4_q_scale(a.scale_log2, a.scale_exp, top);
+#pragma unroll
+    for (int s = 0; s < S; ++s) fp4_q8<QP>(x[s], qs.down, q[s]);
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    sm.init(__builtin_ldexpf(a.scale_log2, a.scale_exp), t.over);
+    sm.init(qs.rm, t.over);
   }
   // Probabilities of a page as planes, from its scores (slots 4 lg + e and 16 + 4
   // lg + e).
@@ -823,13 +851,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
     row.node = r / a.G;
     row.head = t.kvh * a.G + r % a.G;
     const QT* qp = (const QT*)a.q + t.b * a.qsb + row.node * a.qst + (long long)row.head * HD + 8 * h;
+    float x[S][8];
 #pragma unroll
-    for (int s = 0; s < S; ++s) fp4_q8<QT, QP>(qp + 16 * s, a.scale_log2, row.q[s]);
+    for (int s = 0; s < S; ++s) load_q8<QT>(qp + 16 * s, x[s]);
+    unsigned top = top_of(x);
+    top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
+    const QScale qs = fp4_q_scale(a.scale_log2, a.scale_exp, top);
+#pragma unroll
+    for (int s = 0; s < S; ++s) fp4_q8<QP>(x[s], qs.down, row.q[s]);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) row.acc[d][i] = 0.f;
-    row.sm.init(__builtin_ldexpf(a.scale_log2, a.scale_exp), t.over);
+    row.sm.init(qs.rm, t.over);
   }
   // as in fp4_many_kernel (12 chunks of 500 x 4 rows over 1000 in bf16: 183 -> 172 us, one of
   // 1000 alone 33.5 -> 29.6)

@@ -53,6 +53,38 @@ def test_scores_of_ordinary_size_whatever_their_factors(case, kind):
         assert torch.isfinite(out).all()
 
 
+# q . k beyond fp32 or below its normal numbers; subnormal q.
+BEYOND = [(20, 110, 2.0 ** -133), (70, 70, -2.0 ** -143), (-70, -60, 3.3e38), (-64, -60, -2.0 ** 121), (-135, 10, 2.0 ** 122)]
+
+
+@pytest.mark.parametrize("case,kind", params(KERNELS))
+def test_scores_of_ordinary_size_by_way_of_sums_beyond_fp32(case, kind):
+    """Rows of q are as if scaled to entries below 2; what they are times keys below 2^119 is in range."""
+    from paper_2412_10418_amd import binding as bd
+    for of_q, of_k, scale in BEYOND:
+        rng = np.random.default_rng([case.B, case.n, case.hd, 84])
+        cache, lens, some, k, v = _filled(rng, case, of_k)
+        q = (_rows(rng, (case.B, case.n, case.H, case.hd), "f32") * 2.0 ** of_q).to(KIND[kind])
+        parents = np.stack([random_tree(rng, case.n, 3) for _ in range(case.B)])
+        out = bd.cdsl_op_tree_attention(cache, q, _ints(lens), _ints(parents), scale=scale, max_len=case.longest)
+        _check(out[some], q[some], k, v, [lens[b] for b in some], parents[some], [case.n] * len(some), scale,
+               f"{case.name} {kind} {of_q} {of_k} {scale}")
+        assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("case,kind", params(("few1", "few2", "many", "wide", "paired hd32")))
+def test_scaling_a_row_by_powers_of_two_changes_no_bit(case, kind):
+    """q times 2^a under a scale times 2^-a: what is taken of the entries does not depend on their row's size."""
+    from paper_2412_10418_amd import binding as bd
+    rng = np.random.default_rng([case.B, case.n, case.hd, 85])
+    cache, lens, _, _, _ = _filled(rng, case)
+    q = _rows(rng, (case.B, case.n, case.H, case.hd), "f32").to(KIND[kind])
+    ref = bd.cdsl_op_tree_attention(cache, q, _ints(lens), scale=0.125, max_len=case.longest)
+    for a in (-90, -1, 1, 30, 110):
+        got = bd.cdsl_op_tree_attention(cache, q * 2.0 ** a, _ints(lens), scale=0.125 * 2.0 ** -a, max_len=case.longest)
+        assert torch.equal(got, ref), a
+
+
 @pytest.mark.parametrize("scale", [0.0, 1e-8, -1e-30, 1e30, 3e38])
 @pytest.mark.parametrize("case,kind", params(("few1", "few2", "many", "wide", "paired hd32")))
 def test_queries_and_scales_of_any_size(case, kind, scale):
