@@ -10,6 +10,8 @@
 namespace cdsl {
 
 constexpr int kForkRows = 512;      // prompts whose tables one launch forks
+constexpr int kForkThreads = 1024, kForkCols = 4;   // of a workgroup of that launch, at most; columns of the table at a time
+constexpr int kForkGroups = 1 << 16;                // its workgroups, at most: a launch has fewer than 2^32 threads
 constexpr int kPieceWords = 512;    // 16-byte words that a workgroup copies at a time, at most
 
 // Pages that a run of count tokens behind len others reaches: [first, end), cut
@@ -65,6 +67,16 @@ CDSL_KVQ_HD CompactSpace compact_space(int pages) {
   s.moves = s.dst + most;
   s.ints = s.moves + 1;
   return s;
+}
+
+// The launch that forks up to kForkRows prompts: workgroup g takes the columns
+// kForkCols * (g + k * groups), k = 0, 1, ... and those behind.
+struct ForkGrid {
+  int groups, threads;
+};
+CDSL_KVQ_HD ForkGrid fork_grid(int B, int P) {
+  const int threads = (B * kForkCols + 63) / 64 * 64, groups = (P + kForkCols - 1) / kForkCols;
+  return {groups < kForkGroups ? groups : kForkGroups, threads < kForkThreads ? threads : kForkThreads};
 }
 
 // How a page of a layer is cut into pieces of nearly one size.

@@ -28,8 +28,6 @@ __device__ __forceinline__ int parent_entry(const PagesArgs& a, int parent, int 
   return parent >= 0 && parent < a.B ? a.table[(long long)parent * a.P + i] : -1;
 }
 
-constexpr int kForkThreads = 1024, kForkCols = 4;
-
 // Workgroup = four columns of the table, which it holds in LDS, all rows of them,
 // before it writes any: one launch, where a copy of the table takes two.  A thread an
 // entry, as far as they go: loads and atomics that wait for each other bound it (with 16
@@ -38,17 +36,21 @@ constexpr int kForkThreads = 1024, kForkCols = 4;
 __global__ __launch_bounds__(kForkThreads) void fork_kernel(PagesArgs a, const int* parents) {
   constexpr int COLS = kForkCols;
   __shared__ int old[kForkRows * COLS];
-  const int col = threadIdx.x % COLS, i = blockIdx.x * COLS + col, rows = blockDim.x / COLS;
-  if (i < a.P)
-    for (int b = threadIdx.x / COLS; b < a.B; b += rows) old[b * COLS + col] = a.table[(long long)b * a.P + i];
-  __syncthreads();
-  if (i >= a.P) return;
-  for (int b = threadIdx.x / COLS; b < a.B; b += rows) {
-    const int p = parents[b];
-    if (p == b) continue;
-    const int now = p >= 0 && p < a.B ? old[p * COLS + col] : -1;
-    hold(a.refs, a.pages, old[b * COLS + col], now);
-    a.table[(long long)b * a.P + i] = now;
+  const int col = threadIdx.x % COLS, rows = blockDim.x / COLS;
+  for (int c = blockIdx.x * COLS; c < a.P; c += gridDim.x * COLS) {
+    const int i = c + col;
+    if (i < a.P)
+      for (int b = threadIdx.x / COLS; b < a.B; b += rows) old[b * COLS + col] = a.table[(long long)b * a.P + i];
+    __syncthreads();
+    if (i < a.P)
+      for (int b = threadIdx.x / COLS; b < a.B; b += rows) {
+        const int p = parents[b];
+        if (p == b) continue;
+        const int now = p >= 0 && p < a.B ? old[p * COLS + col] : -1;
+        hold(a.refs, a.pages, old[b * COLS + col], now);
+        a.table[(long long)b * a.P + i] = now;
+      }
+    __syncthreads();   // before the next columns take their place
   }
 }
 
@@ -514,8 +516,8 @@ CopyArgs copy_within(const PagesArgs& a, const int* src, const int* dst, const i
 hipError_t pages_fork_launch(const PagesArgs& a, const int* parents, int* workspace, hipStream_t st) {
   if (a.B == 0) return hipSuccess;
   if (a.B <= kForkRows) {
-    const int threads = std::min((a.B * kForkCols + 63) / 64 * 64, kForkThreads);
-    fork_kernel<<<(unsigned)((a.P + kForkCols - 1) / kForkCols), threads, 0, st>>>(a, parents);
+    const ForkGrid g = fork_grid(a.B, a.P);
+    fork_kernel<<<(unsigned)g.groups, g.threads, 0, st>>>(a, parents);
     return hipGetLastError();
   }
   const dim3 grid((unsigned)std::min((a.P + 255) / 256, 64), (unsigned)a.B);
