@@ -599,7 +599,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
   constexpr int ROWS = 16 * W;
   // operands of 64 lanes: keys [S][half], values [S][even, odd]
   __shared__ __attribute__((aligned(16))) u32x4 tile[2][(2 * S + DT) * 64];
-  __shared__ uint8_t gone[2][kPage];     // 1: the slot's value is NaN
+  __shared__ __attribute__((aligned(4))) uint8_t gone[2][kPage];     // 1: the slot's value is NaN; read by words
+  static_assert(__alignof__(gone) >= 4, "words");
   __shared__ uint32_t masks[ROWS * kTreeWords];
   __shared__ int par[kTreeMax];
 
@@ -771,6 +772,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(QT) 
   };
   __shared__ __attribute__((aligned(16))) Tile tiles[2][KS];
   __shared__ __attribute__((aligned(4))) uint8_t gone[2][KS][kPage];     // 1: the slot's value is NaN
+  static_assert(__alignof__(gone) >= 4, "words");
   __shared__ uint32_t masks[ROWS * kTreeWords];
   __shared__ int par[kTreeMax];
   static_assert(KS == 1 || sizeof(tiles) >= TILES * (2 + 16 * DT) * 64 * sizeof(float), "room for the merge");
