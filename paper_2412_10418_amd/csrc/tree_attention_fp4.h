@@ -19,7 +19,9 @@
 // planes, three for fp32, one for bf16: exact down to 2^-103 of the largest entry.
 // Probabilities (1 to 2^8 at most, see kLazy) are planes as over 8 bits: three for fp32;
 // for bf16 two with one tile of rows, and one (2^-8 of each, 0.0023 of the result in the
-// mean square where its own rounding is 0.0017) with more.
+// mean square where its own rounding is 0.0017) with more, where a second costs 6 to 30%
+// (8 prompts of 8 nodes x 4 at 4096: 21.4 -> 23.5 us, 64 trees of 65 at 2048: 121 -> 136,
+// two chunks of 509 over 3001: 67 -> 78, of 512 over 32768: 551 -> 718).
 #pragma once
 #include "tree_attention.h"
 
@@ -378,7 +380,7 @@ struct Fp4Pages {
 // The bytes bound it where keys are long: 8 tokens of up to 32768, 4 query heads each
 // of 8 KV heads, take 35 to 40 us with the merge's 5, and their 160 MB 33 at the rate of
 // a copy.  A token at 256 takes 5.9 us, its start and three dependent loads.  (In fp32
-// two tiles of heads of 128 spill 104 bytes a lane; 8 prompts of 8 x 4 rows at 4096
+// two tiles of heads of 128 spill 128 bytes a lane; 8 prompts of 8 x 4 rows at 4096
 // take 31 us, in bf16 23.)
 template <int HD, typename QT, int RPW>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void fp4_few_kernel(TreeAttnArgs a) {
@@ -751,7 +753,7 @@ struct Fp4Wide {
 // the vector work beside a matrix instruction, which keeps its SIMD from it for
 // about eight cycles whatever its size: two chunks of 512 over 32768 tokens in bf16 take
 // 590 us, 0.94 PFLOP/s, with tiles of 16 847.  (In bf16 three waves a SIMD, which spill
-// 72 bytes a lane.)
+// 84 bytes a lane.)
 // TILES: row tiles of a workgroup, 4 or 2.  With two, a pair of waves shares a
 // tile's rows and takes every other page each; they merge through LDS.  (Two chunks of
 // 509 over 3001, lengths alike, in bf16: 90 us.  Before a CU had groups of either end,

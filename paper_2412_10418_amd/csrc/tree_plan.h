@@ -63,10 +63,11 @@ inline TreeAttnPlan tree_attn_plan(int B, int n, int H, int Hkv, int hd, int max
   //    and 63, 61; over 3001: 85, 76 and 131, 127; over 8192: 240, 198 and 364, 354,
   //    where whole tiles over split keys take 185 and 353; 16 trees of 64 x 4 at
   //    1000: 33, 31 and 47, 45; 16 of 51 at 512: 25.0, 25.4 and 35.4, 36.7);
-  //  - where long keys are split (a chunk of 512 over 32768, two prompts: 847, 580 and
+  //  - where keys are long, mostly to be split (a chunk of 512 over 32768, two prompts: 847, 580 and
   //    1313, 1230; 32 trees of 17 at 8192: 236, 152 and 336, 296; 8 of 65, whose 17
   //    tiles leave the last group part empty: 98, 85 and 145, 154; 4 of 64 at 4000: 38,
-  //    39 and 50, 52);
+  //    39 and 50, 52; whole where the workgroups are too many for two parts a prompt, as
+  //    two chunks of 513 to 672 over 3001 in bf16: 108 to 116, where 512 take 83 in pairs);
   //  - in bf16 where they fill the chip (12 chunks of 500 at 1000: 199, 178 and 330,
   //    343; 64 trees of 64 at 1024: 111, 105 and 191, 190).
   if (format == kMxfp4) {
