@@ -7,7 +7,6 @@
 #include <string.h>
 
 #include <algorithm>
-#include <cfloat>
 #include <cmath>
 #include <mutex>
 #include <new>
